@@ -67,6 +67,34 @@ swarm_status swarm_head_loss_backward(const swarm_head_config *cfg, const swarm_
                                       const swarm_head_grads *grads, void *workspace, size_t workspace_bytes,
                                       void *hip_stream);
 
+/* The logits alone (generation): logits [T, vocab_rows] of `dtype` (overwritten; columns >= vocab are the products with the padding
+ * rows).  Workspace: swarm_head_workspace_bytes(cfg, 0). */
+swarm_status swarm_head_logits(const swarm_head_config *cfg, const swarm_head_params *params, const void *x, void *logits,
+                               void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Rules on rows of logits before a token is chosen.  With x the logit of token v in row r, in fp32:
+ *     n = how often v occurs in history[r, 0 .. history_len[r] - 1]
+ *     if n > 0:  x = x > 0 ? x / repetition[r] : x * repetition[r];   x = x - frequency[r] * n - presence[r]
+ *     x = x + bias[r, i], added up over the i < bias_len[r] with bias_ids[r, i] == v, in the order of i, if there are any
+ *     x = -infinity where bit v % 32 of allowed[r, v / 32] is clear (a grammar's mask; a row may allow nothing)
+ * out [rows, vocab] fp32 (rows out_pitch elements apart, may be `logits` itself where that is fp32 with the same pitch).
+ * history [rows, history_max], bias_ids and bias [rows, bias_max], allowed [rows, ceil(vocab / 32)] are device arrays; history,
+ * bias_ids and allowed may be NULL (no such rule), and so may repetition (1), frequency (0) and presence (0).  Ids outside
+ * [0, vocab) are ignored; a length outside 0 .. its maximum counts as the nearer end.
+ * 1 <= rows <= 65535; 1 <= vocab <= 2^24; 0 <= history_max <= 2^24; 0 <= bias_max <= 1024; pitches >= vocab. */
+typedef struct {
+  int32_t rows, vocab;
+  int32_t history_max, bias_max;
+  const int32_t *history, *history_len;
+  const float *repetition, *frequency, *presence;   /* [rows] */
+  const int32_t *bias_ids;
+  const float *bias;
+  const int32_t *bias_len;
+  const uint32_t *allowed;
+} swarm_logits_rules;
+swarm_status swarm_logits_adjust(const swarm_logits_rules *rules, const void *logits, int32_t dtype, size_t logits_pitch,
+                                 float *out, size_t out_pitch, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

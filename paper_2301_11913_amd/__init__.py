@@ -18,4 +18,8 @@ from .binding import (  # noqa: F401
     swarm_head_loss, swarm_head_loss_backward,
     swarm_lamb_workspace_bytes, swarm_lamb_step, swarm_lamb_step_static, SWARM_LAMB_STATIC_MAX_ELEMS,
     swarm_codec_encode_s16, swarm_codec_decode_s16,
+    CacheConfig, Cache, swarm_cache_append, swarm_cache_read, swarm_cache_keep,
+    swarm_cache_attention_workspace_bytes, swarm_cache_attention,
+    swarm_stage_extend_workspace_bytes, swarm_stage_extend,
+    swarm_head_logits, LogitsRules, swarm_logits_adjust,
 )

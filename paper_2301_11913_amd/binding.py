@@ -1,4 +1,4 @@
-"""ctypes binding of the C ABI in include/swarm_stage.h (argument marshalling only)."""
+"""ctypes binding of the C ABI in include/ (argument marshalling only)."""
 from __future__ import annotations
 
 import contextlib
@@ -21,7 +21,11 @@ EXPORTED_SYMBOLS = ("swarm_stage_workspace_bytes", "swarm_stage_forward", "swarm
                     "swarm_head_loss", "swarm_head_loss_backward",
                     "swarm_lamb_workspace_bytes", "swarm_lamb_step", "swarm_lamb_step_static",
                     "swarm_codec_encode_s16", "swarm_codec_decode_s16",
-                    "swarm_stage_forward_coded_s16", "swarm_stage_backward_coded_s16")
+                    "swarm_stage_forward_coded_s16", "swarm_stage_backward_coded_s16",
+                    "swarm_cache_append", "swarm_cache_read", "swarm_cache_keep",
+                    "swarm_cache_attention_workspace_bytes", "swarm_cache_attention",
+                    "swarm_stage_extend_workspace_bytes", "swarm_stage_extend",
+                    "swarm_head_logits", "swarm_logits_adjust")
 SWARM_COMPRESS_BOTTLENECK, SWARM_COMPRESS_MAXOUT = 0, 1
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -84,6 +88,91 @@ class HeadConfig:
 class _LambConfig(C.Structure):
     _fields_ = [("lr", C.c_float), ("beta1", C.c_float), ("beta2", C.c_float), ("eps", C.c_float),
                 ("weight_decay", C.c_float), ("grad_scale", C.c_float), ("step", C.c_int32)]
+
+
+class _CacheConfig(C.Structure):
+    _fields_ = [("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("d_head", C.c_int32), ("page_tokens", C.c_int32),
+                ("n_pages", C.c_int32), ("batch", C.c_int32), ("table_pages", C.c_int32), ("dtype", C.c_int32),
+                ("scale_bits", C.c_int32)]
+
+
+class _Cache(C.Structure):
+    _fields_ = [("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("k_scales", C.c_void_p), ("v_scales", C.c_void_p)]
+
+
+class CacheConfig:
+    """Host-side description of a paged int8 key / value cache and the sequences in it (mirrors swarm_cache_config)."""
+
+    def __init__(self, n_heads, n_kv_heads, d_head, page_tokens, n_pages, batch, table_pages, dtype, scale_bits=32):
+        if isinstance(dtype, str):
+            dtype = {"f32": SWARM_F32, "bf16": SWARM_BF16}[dtype]
+        elif isinstance(dtype, torch.dtype):
+            dtype = {torch.float32: SWARM_F32, torch.bfloat16: SWARM_BF16}[dtype]
+        self.c = _CacheConfig(n_heads, n_kv_heads, d_head, page_tokens, n_pages, batch, table_pages, dtype, scale_bits)
+        self._ref = C.byref(self.c)
+
+    @property
+    def torch_dtype(self):
+        return torch.float32 if self.c.dtype == SWARM_F32 else torch.bfloat16
+
+    def shapes(self):
+        """Shape and dtype of the four tensors of a Cache (16-bit scales are bf16 values)."""
+        c = self.c
+        scale = torch.float32 if c.scale_bits == 32 else torch.bfloat16
+        return {"k_codes": ((c.n_pages, c.n_kv_heads, c.page_tokens, c.d_head), torch.int8),
+                "v_codes": ((c.n_pages, c.n_kv_heads, c.d_head, c.page_tokens), torch.int8),
+                "k_scales": ((c.n_pages, c.n_kv_heads, c.d_head // 64, c.page_tokens), scale),
+                "v_scales": ((c.n_pages, c.n_kv_heads, c.d_head // 64, c.page_tokens), scale)}
+
+
+class Cache:
+    """The pool of one block application: four tensors as CacheConfig.shapes() says, checked once here."""
+
+    def __init__(self, cfg: CacheConfig, k_codes, v_codes, k_scales, v_scales):
+        self.tensors = {"k_codes": k_codes, "v_codes": v_codes, "k_scales": k_scales, "v_scales": v_scales}
+        for name, (shape, dtype) in cfg.shapes().items():
+            t = self.tensors[name]
+            if tuple(t.shape) != shape:
+                raise ValueError("%s has shape %s, the cache has %s" % (name, tuple(t.shape), shape))
+            if t.dtype != dtype and not (t.element_size() == 2 and dtype == torch.bfloat16):
+                raise TypeError("%s must be %s" % (name, dtype))
+        self.layout = bytes(cfg.c)
+        self.c = _Cache(*(_on_device(t) for t in self.tensors.values()))
+        self._ref = C.byref(self.c)
+
+
+class _LogitsRules(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("vocab", C.c_int32), ("history_max", C.c_int32), ("bias_max", C.c_int32)] + \
+               [(k, C.c_void_p) for k in ("history", "history_len", "repetition", "frequency", "presence", "bias_ids", "bias",
+                                          "bias_len", "allowed")]
+
+
+class LogitsRules:
+    """The rules of swarm_logits_adjust (mirrors swarm_logits_rules); the tensors are kept alive and read at every call.
+    history, bias_ids [rows, n] int32; history_len, bias_len [rows] int32; bias [rows, n] and repetition, frequency, presence [rows]
+    fp32; allowed [rows, ceil(vocab / 32)] int32 (bit patterns)."""
+
+    def __init__(self, rows, vocab, history=None, history_len=None, repetition=None, frequency=None, presence=None, bias_ids=None,
+                 bias=None, bias_len=None, allowed=None):
+        given = dict(history=history, history_len=history_len, repetition=repetition, frequency=frequency, presence=presence,
+                     bias_ids=bias_ids, bias=bias, bias_len=bias_len, allowed=allowed)
+        n_history = history.shape[1] if history is not None else 0
+        n_bias = bias_ids.shape[1] if bias_ids is not None else 0
+        whole = {"history": (rows, n_history), "history_len": (rows,), "bias_ids": (rows, n_bias), "bias_len": (rows,),
+                 "allowed": (rows, (vocab + 31) // 32)}
+        real = {"repetition": (rows,), "frequency": (rows,), "presence": (rows,), "bias": (rows, n_bias)}
+        for name, t in given.items():
+            if t is None:
+                continue
+            if name in whole and (t.dtype not in (torch.int32, getattr(torch, "uint32", torch.int32))):
+                raise TypeError("%s must be int32" % name)
+            if name in real and t.dtype != torch.float32:
+                raise TypeError("%s must be fp32" % name)
+            if tuple(t.shape) != (whole.get(name) or real.get(name)):
+                raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), whole.get(name) or real.get(name)))
+        self.tensors = given
+        self.c = _LogitsRules(rows, vocab, n_history, n_bias, *(_on_device(t) for t in given.values()))
+        self._ref = C.byref(self.c)
 
 
 class StageConfig:
@@ -219,6 +308,25 @@ def _open(path):
     lib.swarm_lamb_step_static.restype = C.c_int
     lib.swarm_lamb_step_static.argtypes = [C.POINTER(_LambConfig), C.c_size_t, C.c_void_p, C.c_void_p, C.c_int32,
                                            C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+    P, I32, SZ = C.c_void_p, C.c_int32, C.c_size_t
+    lib.swarm_cache_append.restype = C.c_int
+    lib.swarm_cache_append.argtypes = [P] * 5 + [I32, P, P, P, SZ, P, I32, P, SZ, P]
+    lib.swarm_cache_read.restype = C.c_int
+    lib.swarm_cache_read.argtypes = [P] * 5 + [I32, P, P, P]
+    lib.swarm_cache_keep.restype = C.c_int
+    lib.swarm_cache_keep.argtypes = [P] * 6 + [I32, P]
+    lib.swarm_cache_attention_workspace_bytes.restype = SZ
+    lib.swarm_cache_attention_workspace_bytes.argtypes = [P, I32, I32]
+    lib.swarm_cache_attention.restype = C.c_int
+    lib.swarm_cache_attention.argtypes = [P] * 5 + [I32, I32, P, SZ, P, P, SZ, P, SZ, P]
+    lib.swarm_stage_extend_workspace_bytes.restype = SZ
+    lib.swarm_stage_extend_workspace_bytes.argtypes = [P, P, I32]
+    lib.swarm_stage_extend.restype = C.c_int
+    lib.swarm_stage_extend.argtypes = [P] * 9 + [I32, P, P, P, SZ, P]
+    lib.swarm_head_logits.restype = C.c_int
+    lib.swarm_head_logits.argtypes = [P] * 5 + [SZ, P]
+    lib.swarm_logits_adjust.restype = C.c_int
+    lib.swarm_logits_adjust.argtypes = [P, P, I32, SZ, P, SZ, P]
     lib.swarm_status_string.restype = C.c_char_p
     lib.swarm_status_string.argtypes = [C.c_int]
     return lib
@@ -234,6 +342,43 @@ def _ptr(t: Optional[torch.Tensor]):
     if not t.is_contiguous():
         raise ValueError("tensors passed to the stage library must be contiguous")
     return t.data_ptr()
+
+
+def _on_device(t: Optional[torch.Tensor]):
+    """_ptr of a tensor that a kernel will read: it has to lie on the current GPU (any tensor where there is no GPU at all)."""
+    if t is None:
+        return None
+    if not t.is_contiguous():
+        raise ValueError("tensors passed to the stage library must be contiguous")
+    if _current_device is not None and torch.cuda.is_initialized() and t.get_device() != _current_device():
+        raise ValueError("a tensor is on %s, the current GPU is %d" % (t.device, _current_device()))
+    return t.data_ptr()
+
+
+def _rows(t: Optional[torch.Tensor], rows: int, width: int, dtype: torch.dtype, name: str):
+    """(pointer, pitch in elements) of a [rows, width] tensor whose rows may lie further apart."""
+    if t is None:
+        return None, 0
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s" % (name, dtype))
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != width:
+        raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), (rows, width)))
+    if width > 1 and t.stride(1) != 1:
+        raise ValueError("the elements of a row of %s must be contiguous" % name)
+    if _current_device is not None and torch.cuda.is_initialized() and t.get_device() != _current_device():
+        raise ValueError("%s is on %s, the current GPU is %d" % (name, t.device, _current_device()))
+    return t.data_ptr(), (t.stride(0) if rows > 1 else max(width, t.stride(0)))
+
+
+def _ints(t: Optional[torch.Tensor], n: int, name: str):
+    """Pointer of a contiguous int32 tensor of n elements."""
+    if t is None:
+        return None
+    if t.dtype != torch.int32:
+        raise TypeError("%s must be int32" % name)
+    if t.numel() != n:
+        raise ValueError("%s has %d elements, expected %d" % (name, t.numel(), n))
+    return _on_device(t)
 
 
 # The current stream's handle without the torch.cuda.Stream object around it, which takes longer to make than a launch (a call
@@ -512,3 +657,147 @@ def swarm_lamb_step_static(master: torch.Tensor, param: Optional[torch.Tensor], 
                                                _ptr(m), _ptr(v), _ptr(trust_ratio), _stream(stream))
     if st != 0:
         raise SwarmError(st, "swarm_lamb_step_static")
+
+
+def _pool(cfg: CacheConfig, cache: Cache):
+    if cache.layout != bytes(cfg.c):
+        a = _CacheConfig.from_buffer_copy(cache.layout)
+        same = ("n_kv_heads", "d_head", "page_tokens", "n_pages", "scale_bits")
+        if any(getattr(a, k) != getattr(cfg.c, k) for k in same):
+            raise ValueError("the cache was made for another configuration")
+    return cache._ref
+
+
+def _tree(tree: Optional[torch.Tensor], rows: int):
+    if tree is None:
+        return None
+    if tree.dtype not in (torch.int64, getattr(torch, "uint64", torch.int64)):
+        raise TypeError("tree must be a 64-bit tensor")
+    if tree.numel() != rows:
+        raise ValueError("tree has %d words, expected %d" % (tree.numel(), rows))
+    return _on_device(tree)
+
+
+def swarm_cache_append(cfg: CacheConfig, cache: Cache, page_table: torch.Tensor, past: torch.Tensor,
+                       fresh: Optional[torch.Tensor], tokens: int, k: torch.Tensor, v: torch.Tensor,
+                       q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                       positions: Optional[torch.Tensor] = None, rotary: bool = False, stream=None) -> None:
+    """q, k, v: [batch * tokens, heads * d_head] views of one row pitch (the columns of a fused product)."""
+    c = cfg.c
+    rows, dt = c.batch * tokens, cfg.torch_dtype
+    kp, pitch = _rows(k, rows, c.n_kv_heads * c.d_head, dt, "k")
+    vp, v_pitch = _rows(v, rows, c.n_kv_heads * c.d_head, dt, "v")
+    qp, q_pitch = _rows(q, rows, c.n_heads * c.d_head, dt, "q")
+    op, out_pitch = _rows(q_out, rows, c.n_heads * c.d_head, dt, "q_out")
+    if rows == 1:                       # a single row has no pitch
+        pitch = v_pitch = q_pitch = max(pitch, v_pitch, q_pitch)
+    if v_pitch != pitch or (q is not None and q_pitch != pitch):
+        raise ValueError("q, k and v must have the same row pitch")
+    st = load_library().swarm_cache_append(cfg._ref, _pool(cfg, cache), _ints(page_table, c.batch * c.table_pages, "page_table"),
+                                           _ints(past, c.batch, "past"), _ints(fresh, c.batch, "fresh"), tokens, qp, kp, vp, pitch,
+                                           _ints(positions, rows, "positions"), int(rotary), op, out_pitch, _stream(stream))
+    if st != 0:
+        raise SwarmError(st, "swarm_cache_append")
+
+
+def swarm_cache_read(cfg: CacheConfig, cache: Cache, page_table: torch.Tensor, first: torch.Tensor,
+                     count: Optional[torch.Tensor], tokens: int, k_out: torch.Tensor, v_out: torch.Tensor, stream=None) -> None:
+    c = cfg.c
+    for t in (k_out, v_out):
+        if t.dtype != cfg.torch_dtype:
+            raise TypeError("k_out and v_out must be %s" % cfg.torch_dtype)
+        if t.numel() != c.batch * tokens * c.n_kv_heads * c.d_head:
+            raise ValueError("k_out and v_out must have batch * tokens rows of n_kv_heads * d_head elements")
+    st = load_library().swarm_cache_read(cfg._ref, _pool(cfg, cache), _ints(page_table, c.batch * c.table_pages, "page_table"),
+                                         _ints(first, c.batch, "first"), _ints(count, c.batch, "count"), tokens,
+                                         _on_device(k_out), _on_device(v_out), _stream(stream))
+    if st != 0:
+        raise SwarmError(st, "swarm_cache_read")
+
+
+def swarm_cache_keep(cfg: CacheConfig, cache: Cache, page_table: torch.Tensor, past: torch.Tensor, kept: torch.Tensor,
+                     n_kept: torch.Tensor, tokens: int, stream=None) -> None:
+    c = cfg.c
+    st = load_library().swarm_cache_keep(cfg._ref, _pool(cfg, cache), _ints(page_table, c.batch * c.table_pages, "page_table"),
+                                         _ints(past, c.batch, "past"), _ints(kept, c.batch * tokens, "kept"),
+                                         _ints(n_kept, c.batch, "n_kept"), tokens, _stream(stream))
+    if st != 0:
+        raise SwarmError(st, "swarm_cache_keep")
+
+
+def swarm_cache_attention_workspace_bytes(cfg: CacheConfig, tokens: int, max_len: int = 0) -> int:
+    return int(load_library().swarm_cache_attention_workspace_bytes(cfg._ref, tokens, max_len))
+
+
+def swarm_cache_attention(cfg: CacheConfig, cache: Cache, page_table: torch.Tensor, past: torch.Tensor,
+                          fresh: Optional[torch.Tensor], tokens: int, q: torch.Tensor, out: torch.Tensor,
+                          workspace: Optional[torch.Tensor], tree: Optional[torch.Tensor] = None, max_len: int = 0,
+                          stream=None) -> None:
+    """q, out: [batch * tokens, n_heads * d_head]; their rows may lie further apart."""
+    c = cfg.c
+    rows, width, dt = c.batch * tokens, c.n_heads * c.d_head, cfg.torch_dtype
+    qp, q_pitch = _rows(q, rows, width, dt, "q")
+    op, out_pitch = _rows(out, rows, width, dt, "out")
+    n = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    st = load_library().swarm_cache_attention(cfg._ref, _pool(cfg, cache), _ints(page_table, c.batch * c.table_pages, "page_table"),
+                                              _ints(past, c.batch, "past"), _ints(fresh, c.batch, "fresh"), tokens, max_len, qp,
+                                              q_pitch, _tree(tree, rows), op, out_pitch, _on_device(workspace) if n else None, n,
+                                              _stream(stream))
+    if st != 0:
+        raise SwarmError(st, "swarm_cache_attention")
+
+
+def swarm_stage_extend_workspace_bytes(cfg: StageConfig, cache_cfg: CacheConfig, max_len: int = 0) -> int:
+    return int(load_library().swarm_stage_extend_workspace_bytes(C.byref(cfg.c), cache_cfg._ref, max_len))
+
+
+def swarm_stage_extend(cfg: StageConfig, params: List[Dict[str, torch.Tensor]], cache_cfg: CacheConfig, caches: Sequence[Cache],
+                       page_table: torch.Tensor, past: torch.Tensor, fresh: Optional[torch.Tensor], x_in: torch.Tensor,
+                       x_out: torch.Tensor, workspace: torch.Tensor, positions: Optional[torch.Tensor] = None,
+                       tree: Optional[torch.Tensor] = None, max_len: int = 0, stream=None) -> None:
+    """caches: one for each of the n_layers * n_repeat applications, in their order."""
+    c, cc = cfg.c, cache_cfg.c
+    rows = c.batch * c.seq
+    if len(params) != c.n_layers or len(caches) != c.n_layers * c.n_repeat:
+        raise ValueError("the stage has %d parameter sets and %d applications" % (c.n_layers, c.n_layers * c.n_repeat))
+    for t in (x_in, x_out):
+        if t.dtype != cfg.torch_dtype or t.numel() != rows * c.d_model:
+            raise ValueError("x_in and x_out must be [batch * seq, d_model] of the stage's dtype")
+    for pool in caches:
+        _pool(cache_cfg, pool)
+    pools = (_Cache * len(caches))(*(pool.c for pool in caches))
+    st = load_library().swarm_stage_extend(C.byref(c), _block_array(params), cache_cfg._ref, pools,
+                                           _ints(page_table, cc.batch * cc.table_pages, "page_table"),
+                                           _ints(past, cc.batch, "past"), _ints(fresh, cc.batch, "fresh"),
+                                           _ints(positions, rows, "positions"), _tree(tree, rows), max_len, _on_device(x_in),
+                                           _on_device(x_out), _on_device(workspace), workspace.numel() * workspace.element_size(),
+                                           _stream(stream))
+    if st != 0:
+        raise SwarmError(st, "swarm_stage_extend")
+
+
+def swarm_head_logits(cfg: HeadConfig, params: Dict[str, torch.Tensor], x: torch.Tensor, logits: torch.Tensor,
+                      workspace: torch.Tensor, stream=None) -> None:
+    if logits.dtype != x.dtype or _dtype_code(x) != cfg.c.dtype:
+        raise TypeError("x and logits must have the head's dtype")
+    if x.numel() != cfg.c.tokens * cfg.c.d_model or logits.numel() != cfg.c.tokens * cfg.c.vocab_rows:
+        raise ValueError("x must be [tokens, d_model] and logits [tokens, vocab_rows]")
+    st = load_library().swarm_head_logits(C.byref(cfg.c), C.byref(_ptrs3(params, "w_vocab")), _on_device(x), _on_device(logits),
+                                          _on_device(workspace), workspace.numel() * workspace.element_size(), _stream(stream))
+    if st != 0:
+        raise SwarmError(st, "swarm_head_logits")
+
+
+def swarm_logits_adjust(rules: LogitsRules, logits: torch.Tensor, out: torch.Tensor, stream=None) -> None:
+    """logits [rows, >= vocab] fp32 or bf16, out [rows, >= vocab] fp32; rows may lie further apart."""
+    rows, vocab = rules.c.rows, rules.c.vocab
+    if out.dtype != torch.float32:
+        raise TypeError("out must be fp32")
+    for name, t in (("logits", logits), ("out", out)):
+        if t.dim() != 2 or t.shape[0] != rows or t.shape[1] < vocab:
+            raise ValueError("%s must be [rows, vocab or more]" % name)
+    lp, pitch = _rows(logits, rows, logits.shape[1], logits.dtype, "logits")
+    op, out_pitch = _rows(out, rows, out.shape[1], out.dtype, "out")
+    st = load_library().swarm_logits_adjust(rules._ref, lp, _dtype_code(logits), pitch, op, out_pitch, _stream(stream))
+    if st != 0:
+        raise SwarmError(st, "swarm_logits_adjust")

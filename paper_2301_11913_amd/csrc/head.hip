@@ -254,16 +254,23 @@ size_t plan(const swarm_head_config* c, bool backward, void* ws, Plan& P) {
 swarm_status gemm(bool bf16, const GemmArgs& g, hipStream_t st) { return bf16 ? gemm_bf16(g, st) : gemm_f32(g, st); }
 bool al16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
+// n = LayerNorm(x), logits [T, Vp] = n W^T
+swarm_status head_products(const swarm_head_config* cfg, const swarm_head_params* p, const void* x, const Plan& P, hipStream_t st) {
+  const bool bf16 = cfg->dtype == SWARM_BF16;
+  const int T = cfg->tokens, d = cfg->d_model, Vp = cfg->vocab_rows;
+  SWARM_TRY(layernorm_fwd(x, p->ln_g, p->ln_b, P.n, P.mean, P.rstd, T, d, cfg->ln_eps, bf16, st));
+  GemmArgs l{};
+  l.M = T; l.N = Vp; l.K = d; l.A = P.n; l.lda = d; l.B = p->w_vocab; l.ldb = d; l.C = P.logits; l.ldc = Vp;
+  l.epilogue = EPI_STORE;
+  return gemm(bf16, l, st);
+}
+
 swarm_status run_head(const swarm_head_config* cfg, const swarm_head_params* p, const void* x, const int32_t* targets,
                       float* loss, float* token_loss, void* dx, const swarm_head_grads* grads, const Plan& P,
                       hipStream_t st) {
   const bool bf16 = cfg->dtype == SWARM_BF16, backward = dx != nullptr;
   const int T = cfg->tokens, d = cfg->d_model, Vp = cfg->vocab_rows;
-  SWARM_TRY(layernorm_fwd(x, p->ln_g, p->ln_b, P.n, P.mean, P.rstd, T, d, cfg->ln_eps, bf16, st));
-  GemmArgs l{};   // logits [T, Vp] = n W^T
-  l.M = T; l.N = Vp; l.K = d; l.A = P.n; l.lda = d; l.B = p->w_vocab; l.ldb = d; l.C = P.logits; l.ldc = Vp;
-  l.epilogue = EPI_STORE;
-  SWARM_TRY(gemm(bf16, l, st));
+  SWARM_TRY(head_products(cfg, p, x, P, st));
   float* tok = token_loss ? token_loss : P.tok;
   const float inv_T = 1.0f / (float)T;
   if (bf16) {
@@ -353,6 +360,18 @@ extern "C" swarm_status swarm_head_loss(const swarm_head_config* cfg, const swar
   Plan P;
   if (plan(cfg, false, workspace, P) > workspace_bytes) return SWARM_ERR_WORKSPACE;
   return run_head(cfg, p, x, targets, loss, token_loss, nullptr, nullptr, P, (hipStream_t)hip_stream);
+}
+
+extern "C" swarm_status swarm_head_logits(const swarm_head_config* cfg, const swarm_head_params* p, const void* x,
+                                          void* logits, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (!cfg || !p || !x || !logits || !workspace || !p->ln_g || !p->ln_b || !p->w_vocab) return SWARM_ERR_NULL;
+  if (cfg->dtype != SWARM_F32 && cfg->dtype != SWARM_BF16) return SWARM_ERR_DTYPE;
+  if (!valid(cfg)) return SWARM_ERR_SHAPE;
+  if (logits == x || !al16(x) || !al16(logits) || ((uintptr_t)workspace & 255)) return SWARM_ERR_SHAPE;
+  Plan P;
+  if (plan(cfg, false, workspace, P) > workspace_bytes) return SWARM_ERR_WORKSPACE;
+  P.logits = logits;
+  return head_products(cfg, p, x, P, (hipStream_t)hip_stream);
 }
 
 extern "C" swarm_status swarm_head_loss_backward(const swarm_head_config* cfg, const swarm_head_params* p,

@@ -4,7 +4,7 @@
 #include <algorithm>
 #include <cstdlib>
 
-#include "kernels.h"
+#include "cache.h"
 
 namespace swarm {
 
@@ -109,9 +109,20 @@ struct Boundary {
   bool scales16 = false;   // block scales are bf16 bit patterns instead of fp32
 };
 
+// Attention over a cache of earlier tokens instead of the microbatch alone (swarm_stage_extend).
+struct CacheStep {
+  const swarm_cache_config* cfg;
+  CacheArgs cache;             // this application's pool
+  const int32_t* positions;
+  const uint64_t* tree;
+  int max_len;
+  void* scratch;
+};
+
 // y = block(x): writes every intermediate into `s`; the last GEMM is skipped when y == nullptr.
 swarm_status block_forward(const Dims& D, const swarm_block_params& p, const Saved& s, void* y, float eps,
-                           hipStream_t st, const Boundary& bd = Boundary(), bool want_u = true) {
+                           hipStream_t st, const Boundary& bd = Boundary(), bool want_u = true,
+                           const CacheStep* step = nullptr) {
   const int T = D.T, d = D.d, f = D.f;
   if (bd.in_codes)
     SWARM_TRY(layernorm_fwd_decode(bd.in_codes, bd.in_scales, const_cast<void*>(s.x), p.ln1_g, p.ln1_b, s.a, s.mean1,
@@ -121,7 +132,13 @@ swarm_status block_forward(const Dims& D, const swarm_block_params& p, const Sav
   GemmArgs q{};
   q.M = T; q.N = 3 * d; q.K = d; q.A = s.a; q.lda = d; q.B = p.w_qkv; q.ldb = d; q.C = s.qkv; q.ldc = 3 * d;
   q.epilogue = EPI_BIAS; q.bias = p.b_qkv;
-  if (D.rope_geglu) {
+  if (step) {
+    // the append rotates: positions differ from row to row, and its keys go into the cache without a rounding in between
+    SWARM_TRY(gemm(D, q, st));
+    const char* qkv = (const char*)s.qkv;
+    SWARM_TRY(cache_append_launch(step->cfg, step->cache, D.rope_geglu ? qkv : nullptr, qkv + d * D.es, qkv + 2 * d * D.es, 3 * d,
+                                  step->positions, D.rope_geglu, D.rope_geglu ? s.qkv : nullptr, 3 * d, st));
+  } else if (D.rope_geglu) {
     // rotary in the QKV epilogue (fp32, before the rounding to bf16) where the MFMA GEMM takes the shape
     swarm_status fused = SWARM_ERR_SHAPE;
     if (D.bf16) {
@@ -138,7 +155,10 @@ swarm_status block_forward(const Dims& D, const swarm_block_params& p, const Sav
   } else {
     SWARM_TRY(gemm(D, q, st));
   }
-  SWARM_TRY(attention_fwd(s.qkv, s.o, s.lse, D.B, D.S, D.H, D.dh, D.bf16, st));
+  if (step)
+    SWARM_TRY(cache_attention_launch(step->cfg, step->cache, step->max_len, s.qkv, 3 * d, step->tree, s.o, d, step->scratch, st));
+  else
+    SWARM_TRY(attention_fwd(s.qkv, s.o, s.lse, D.B, D.S, D.H, D.dh, D.bf16, st));
   GemmArgs o{};
   o.M = T; o.N = d; o.K = d; o.A = s.o; o.lda = d; o.B = p.w_o; o.ldb = d; o.C = s.h; o.ldc = d;
   o.epilogue = EPI_BIAS_RESID; o.bias = p.b_o; o.aux = s.x; o.ldaux = d;
@@ -469,8 +489,6 @@ bool params_ok(const swarm_block_params* p, int L) {
   return true;
 }
 
-bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
-
 }  // namespace
 }  // namespace swarm
 
@@ -661,4 +679,67 @@ extern "C" swarm_status swarm_stage_backward_coded_s16(const swarm_stage_config*
                                                        void* workspace, size_t workspace_bytes, void* hip_stream) {
   return backward_coded(cfg, params, x_in, g_codes, g_scales, gin_codes, gin_scales, grad_params, workspace,
                         workspace_bytes, hip_stream, true);
+}
+
+// ---------------------------------------------------------------------------------------------
+// New tokens over the caches of earlier ones: the forward call's sequence of launches with the append and the cache's attention in
+// place of the rotation and the microbatch's attention.
+namespace swarm {
+namespace {
+struct ExtendPlan {
+  FwdPlan fwd;
+  void* scratch;       // of the attention
+};
+size_t plan_extend(const Dims& D, const swarm_cache_config* cc, int max_len, void* ws, ExtendPlan& P) {
+  const size_t base = plan_forward(D, ws, P.fwd), need = cache_attention_scratch_bytes(cc, D.S, max_len);
+  P.scratch = need && ws ? (char*)ws + base : nullptr;
+  return base + ((need + 255) & ~(size_t)255);
+}
+bool extend_config_ok(const swarm_stage_config* c, const swarm_cache_config* cc, int max_len) {
+  return valid_config(c) && cache_config_status(cc, c->seq) == SWARM_OK && max_len >= 0 && cc->batch == c->batch &&
+         cc->dtype == c->dtype && cc->n_heads == c->n_heads && cc->n_kv_heads == c->n_heads && cc->d_head == c->d_model / c->n_heads;
+}
+}  // namespace
+}  // namespace swarm
+
+extern "C" size_t swarm_stage_extend_workspace_bytes(const swarm_stage_config* cfg, const swarm_cache_config* cache_cfg,
+                                                     int32_t max_len) {
+  if (!extend_config_ok(cfg, cache_cfg, max_len)) return 0;
+  ExtendPlan P;
+  return plan_extend(dims_of(cfg), cache_cfg, max_len, nullptr, P);
+}
+
+extern "C" swarm_status swarm_stage_extend(const swarm_stage_config* cfg, const swarm_block_params* params,
+                                           const swarm_cache_config* cache_cfg, const swarm_cache* caches,
+                                           const int32_t* page_table, const int32_t* past, const int32_t* fresh,
+                                           const int32_t* positions, const uint64_t* tree, int32_t max_len, const void* x_in,
+                                           void* x_out, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (!cfg || !params || !cache_cfg || !caches || !page_table || !past || !x_in || !x_out || !workspace) return SWARM_ERR_NULL;
+  if ((cfg->dtype != SWARM_F32 && cfg->dtype != SWARM_BF16) || (cache_cfg->dtype != SWARM_F32 && cache_cfg->dtype != SWARM_BF16))
+    return SWARM_ERR_DTYPE;
+  if (!extend_config_ok(cfg, cache_cfg, max_len)) return SWARM_ERR_SHAPE;
+  Dims D = dims_of(cfg);
+  if (!params_ok(params, cfg->n_layers)) return SWARM_ERR_NULL;
+  for (int i = 0; i < D.apps; ++i)
+    if (!cache_pointers_ok(&caches[i])) return SWARM_ERR_NULL;
+  for (int i = 0; i < D.apps; ++i)
+    if (!cache_aligned(&caches[i])) return SWARM_ERR_SHAPE;
+  if (x_in == x_out || !aligned16(x_in) || !aligned16(x_out) || ((uintptr_t)workspace & 255) || ((uintptr_t)tree & 7) ||
+      (tree && D.S > 64) || (positions && !D.rope_geglu))
+    return SWARM_ERR_SHAPE;
+  ExtendPlan P;
+  if (plan_extend(D, cache_cfg, max_len, workspace, P) > workspace_bytes) return SWARM_ERR_WORKSPACE;
+  D.splitk = P.fwd.splitk; D.splitk_floats = P.fwd.splitk ? splitk_floats_of(D) : 0;
+  const void* cur = x_in;
+  int app = 0;
+  for (int l = 0; l < cfg->n_layers; ++l)
+    for (int r = 0; r < cfg->n_repeat; ++r, ++app) {
+      const CacheStep step{cache_cfg, cache_args(cache_cfg, &caches[app], page_table, past, fresh, D.S), positions, tree, max_len,
+                           P.scratch};
+      void* y = (app == D.apps - 1) ? x_out : P.fwd.z[app & 1];
+      P.fwd.s.x = cur;
+      SWARM_TRY(block_forward(D, params[l], P.fwd.s, y, cfg->ln_eps, (hipStream_t)hip_stream, Boundary(), false, &step));
+      cur = y;
+    }
+  return SWARM_OK;
 }
