@@ -1,11 +1,29 @@
-// Attention of new tokens over the paged int8 cache.
+// Attention of new tokens over the paged int8 cache, for few rows per key / value head and for fp32: products of whole numbers.
 //
-// One wavefront per (row, query head), 64 cached tokens at a time: a lane makes one token's score, then owns d_head / 64 elements of
-// the output.  One pass with the running maximum and sum of the softmax.
+// The cache's codes go to the matrix cores as they are.  q is a block's power of two times a whole number of 22 (bf16) or 30 (fp32)
+// bits, and that is a sum of 3 or 4 signed bytes times 256^i: four rows of an int8 MFMA (v_mfma_i32_16x16x64_i8, whose 64 steps of
+// the contraction are exactly one block of the codec) hold one query's bytes, a tile of 16 rows four queries.  The products and their sums are
+// exact; a block's sum is put together from its bytes' sums in fp32 and multiplied by q's power of two and the keys' scales.
+// The weights p_j = 2^(s_j - m) go the same way: p_j times the value's scale, as a whole number of 22 / 30 bits relative to
+// the tile's largest scale, contracted with the value codes over 64 tokens at a time.  Nothing is converted per cached element, and
+// one query uses the matrix cores no worse than four.
+//   keys    column n of tile c is token 4 n + c: a lane then holds the weights of four consecutive tokens, one word per byte row.
+//   values  lie transposed in the cache: a lane's operand is 16 consecutive tokens of one element, one load.
+// What a wavefront reads goes straight into registers, the next 64 tokens' keys while this tile's softmax runs, the next values behind its
+// last product.  Bound by reading the cache while a key / value head has few rows: 16 KB per 64 tokens at d_head 128 against
+// some 300 vector instructions for four rows.  The four wavefronts of a workgroup take tiles in turn; long sequences are spread over
+// workgroups (splits of `chunk` tiles), whose partial sums a second kernel joins.
 #include "cache.h"
 
 namespace swarm {
 namespace {
+
+typedef __attribute__((ext_vector_type(4))) int i32x4;
+
+constexpr int kThreads = 256, kWaves = 4;
+constexpr int kTile = 64;
+constexpr int kRowPitch = 20;          // 32-bit words of a row of weights' bytes: 16, and 4 against bank conflicts
+constexpr float kLog2e = 1.4426950408889634f;
 
 struct AttnArgs {
   CacheArgs c;
@@ -13,80 +31,415 @@ struct AttnArgs {
   void* out;
   const uint64_t* tree;
   size_t q_pitch, out_pitch;
+  float *part_o, *part_ml;     // splits > 1: [unit][rows][d_head], [unit][rows][2]
+  int group;                   // query heads per key / value head
+  int row_groups, splits, chunk;
   bool s16;
 };
 
-template <typename T, int DH>
-__global__ __launch_bounds__(64) void cache_attention_kernel(AttnArgs a) {
-  __shared__ float qs[DH];
-  __shared__ float ps[64];
-  __shared__ int pages[64];
-  const int lane = threadIdx.x, h = blockIdx.x % a.c.H, row = blockIdx.x / a.c.H;
-  const int b = row / a.c.tokens, t = row - b * a.c.tokens, g = h / (a.c.H / a.c.KV);
+// Reductions over the 16 lanes of a row of the register file
+template <int N>
+__device__ __forceinline__ uint32_t turned(uint32_t v) { return __builtin_amdgcn_mov_dpp(v, 0x120 + N, 0xF, 0xF, true); }
+__device__ __forceinline__ float max16(float v) {
+  v = fmaxf(v, __uint_as_float(turned<8>(__float_as_uint(v))));
+  v = fmaxf(v, __uint_as_float(turned<4>(__float_as_uint(v))));
+  v = fmaxf(v, __uint_as_float(turned<2>(__float_as_uint(v))));
+  return fmaxf(v, __uint_as_float(turned<1>(__float_as_uint(v))));
+}
+__device__ __forceinline__ uint32_t umax16(uint32_t v) {
+  v = max(v, turned<8>(v)); v = max(v, turned<4>(v)); v = max(v, turned<2>(v));
+  return max(v, turned<1>(v));
+}
+__device__ __forceinline__ float sum16(float v) {
+  v += __uint_as_float(turned<8>(__float_as_uint(v))); v += __uint_as_float(turned<4>(__float_as_uint(v)));
+  v += __uint_as_float(turned<2>(__float_as_uint(v)));
+  return v + __uint_as_float(turned<1>(__float_as_uint(v)));
+}
+
+// A number below 2^BITS in magnitude as bytes: sum of (signed byte i) * 256^i.
+template <int BYTES>
+__device__ __forceinline__ uint32_t digits(int x) {
+  constexpr uint32_t h = BYTES == 4 ? 0x80808080u : 0x00808080u;
+  const uint32_t w = ((uint32_t)x + h) ^ h;
+  return BYTES == 4 ? w : w & 0x00FFFFFFu;
+}
+// and back, from the sums over the bytes
+template <int BYTES>
+__device__ __forceinline__ float joined(const i32x4& a) {
+  if constexpr (BYTES == 4) return fmaf((float)((a[3] << 8) + a[2]), 65536.0f, (float)((a[1] << 8) + a[0]));
+  return fmaf((float)((a[2] << 8) + a[1]), 256.0f, (float)a[0]);
+}
+
+template <bool S16>
+__device__ __forceinline__ float4 scales4(const void* p, size_t i) {
+  if constexpr (S16) {
+    const uint2 v = *reinterpret_cast<const uint2*>(reinterpret_cast<const uint16_t*>(p) + i);
+    return make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xFFFF0000u), __uint_as_float(v.y << 16),
+                       __uint_as_float(v.y & 0xFFFF0000u));
+  } else {
+    return *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p) + i);
+  }
+}
+
+// RT tiles of four rows; a row is (token t, query head of the group): r = t * group + head.
+template <typename T, int DH, int RT, bool S16>
+__global__ __launch_bounds__(kThreads) void cache_attention_bytes_kernel(AttnArgs a) {
+  constexpr int BYTES = sizeof(T) == 2 ? 3 : 4;
+  constexpr int BITS = BYTES == 4 ? 30 : 22;
+  constexpr int NB = DH / 64, Q = 4 * RT, DT = DH / 16;
+  constexpr int kQBytes = Q * 4 * DH, kOBytes = kWaves * Q * (DH + 2) * 4, kPBytes = kWaves * NB * 16 * kRowPitch * 4;
+  __shared__ __attribute__((aligned(16))) char lds[kQBytes + kPBytes > kOBytes ? kQBytes + kPBytes : kOBytes];
+  __shared__ float q_scale[Q][NB];
+  const int lane = threadIdx.x & 63, n = lane & 15, lg = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);      // the same for all lanes: loops and branches on it are scalar
+  int unit = blockIdx.x;
+  const int split = unit % a.splits; unit /= a.splits;
+  const int g = unit % a.c.KV; unit /= a.c.KV;
+  const int rg = unit % a.row_groups, b = unit / a.row_groups;
   const Span s = span_of(a.c, b);
-  if (t >= s.fresh) return;
-  for (int d = lane; d < DH; d += 64) qs[d] = Elem<T>::load((const T*)a.q + (size_t)row * a.q_pitch + (size_t)h * DH + d);
-  __syncthreads();
-  const uint64_t tree = a.tree ? a.tree[row] : 0;
-  const float c = (DH == 64 ? 0.125f : 0.08838834764831845f) * 1.4426950408889634f;
-  const int n = s.past + s.fresh, P1 = (1 << a.c.page_shift) - 1;
-  float m = -INFINITY, l = 0.f, o[DH / 64] = {};
-  for (int j0 = 0; j0 < n; j0 += 64) {
-    const int j = j0 + lane, u = j - s.past;
-    const int page = j < n ? page_of(a.c, b, j) : -1;
-    const bool sees = page >= 0 && (u < 0 || (a.tree ? (tree >> u) & 1 : u <= t));
-    float x = -INFINITY;
-    if (sees) {
-      const int8_t* k = a.c.k_codes + codes_at<DH>(a.c, page, g) + (size_t)(j & P1) * DH;
-      x = 0.f;
-      for (int blk = 0; blk < DH / 64; ++blk) {
-        float dot = 0.f;
-        for (int d = 0; d < 64; ++d) dot = fmaf((float)k[blk * 64 + d], qs[blk * 64 + d], dot);
-        x = fmaf(dot, block_scale_load(a.c.k_scales, scales_at<DH>(a.c, page, g) + ((size_t)blk << a.c.page_shift) + (j & P1), a.s16), x);
+  const int r0 = rg * Q, rows = s.fresh * a.group;
+  if (r0 >= rows) return;
+  const int t_last = min(r0 + Q, rows) - 1;
+  const int len = a.tree ? s.past + s.fresh : s.past + t_last / a.group + 1;     // tokens that any of these rows sees
+  const int tiles = (len + kTile - 1) / kTile;
+  const int first = split * a.chunk, end = split + 1 == a.splits ? tiles : min(tiles, first + a.chunk);
+
+  // ---- the queries' bytes: 16 lanes make one block of one row
+  {
+    uint8_t* qd = reinterpret_cast<uint8_t*>(lds);
+    for (int i = threadIdx.x; i < Q * NB * 16; i += kThreads) {
+      const int e = i & 15, blk = (i >> 4) % NB, q = (i >> 4) / NB, r = r0 + q;
+      float x[4] = {0.f, 0.f, 0.f, 0.f};
+      if (r < rows) {
+        const T* src = reinterpret_cast<const T*>(a.q) + ((size_t)b * a.c.tokens + r / a.group) * a.q_pitch +
+                       (size_t)(g * a.group + r % a.group) * DH + blk * 64 + e * 4;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) x[u] = Elem<T>::load(src + u);
       }
-      x *= c;
-    }
-    const float mn = fmaxf(m, wave_max(x)), top = mn == -INFINITY ? 0.f : mn;
-    const float keep = exp2f(m - top), p = exp2f(x - top);
-    l = l * keep + wave_sum(p);
-    m = mn;
-    __syncthreads();
-    ps[lane] = sees ? p : 0.f;
-    pages[lane] = sees ? page : -1;
-    __syncthreads();
-    for (int blk = 0; blk < DH / 64; ++blk) {
-      float acc = o[blk] * keep;
-      for (int e = 0; e < 64; ++e) {
-        const int pg = pages[e], place = (j0 + e) & P1;
-        if (pg < 0) continue;
-        const float v = (float)a.c.v_codes[codes_at<DH>(a.c, pg, g) + ((size_t)(blk * 64 + lane) << a.c.page_shift) + place];
-        acc = fmaf(ps[e] * v, block_scale_load(a.c.v_scales, scales_at<DH>(a.c, pg, g) + ((size_t)blk << a.c.page_shift) + place, a.s16), acc);
+      uint32_t top = 0;                 // magnitudes compare as whole numbers, what is no number above all
+#pragma unroll
+      for (int u = 0; u < 4; ++u) top = max(top, __float_as_uint(x[u]) & 0x7FFFFFFFu);
+      top = umax16(top);
+      const int ex = (int)(top >> 23) - 126;                  // magnitudes are below 2^ex
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const uint32_t w = digits<BYTES>((int)rintf(ldexpf(x[u], BITS - ex)));
+#pragma unroll
+        for (int k = 0; k < 4; ++k) qd[(q * 4 + k) * DH + blk * 64 + e * 4 + u] = (uint8_t)(w >> (8 * k));
       }
-      o[blk] = acc;
+      const float c = (DH == 64 ? 0.125f : 0.08838834764831845f) * kLog2e;
+      if (e == 0) q_scale[q][blk] = top >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : ldexpf(c, ex - BITS);
     }
   }
-  for (int blk = 0; blk < DH / 64; ++blk)
-    Elem<T>::store((T*)a.out + (size_t)row * a.out_pitch + (size_t)h * DH + blk * 64 + lane, l == 0.f ? 0.f : o[blk] / l);
+  __syncthreads();
+  i32x4 qf[RT][NB];
+  float qs[RT][NB];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+    for (int blk = 0; blk < NB; ++blk) {
+      qf[rt][blk] = *reinterpret_cast<const i32x4*>(lds + (rt * 16 + n) * DH + blk * 64 + lg * 16);
+      qs[rt][blk] = q_scale[rt * 4 + lg][blk];
+    }
+  uint32_t* weights = reinterpret_cast<uint32_t*>(lds + kQBytes) + wave * NB * 16 * kRowPitch;
+
+  float m[RT], l[RT], o[RT][DT];
+  uint64_t see[RT];
+  int my_t[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    m[rt] = -INFINITY; l[rt] = 0.f;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) o[rt][d] = 0.f;
+    const int r = r0 + rt * 4 + lg;
+    my_t[rt] = r < rows ? r / a.group : 0;
+    see[rt] = a.tree && r < rows ? a.tree[(size_t)b * a.c.tokens + my_t[rt]] : 0;
+  }
+
+  const int P1 = (1 << a.c.page_shift) - 1;
+  const int last_k = (len - 1) & ~3, last_v = (len - 1) & ~15;
+  // pages of the tokens that this lane loads of a tile: keys 4 n .. 4 n + 3, values 16 lg .. 16 lg + 15; past the end the last ones
+  auto page_k = [&](int tile) { return page_of(a.c, b, min(tile * kTile + 4 * n, last_k)); };
+  auto page_v = [&](int tile) { return page_of(a.c, b, min(tile * kTile + 16 * lg, last_v)); };
+  uint4 kf[4][NB], vf[DT];
+  float4 ks[NB], vs[NB];
+  auto load_keys = [&](int tile, int page) {
+    const int place = min(tile * kTile + 4 * n, last_k) & P1;
+    const int8_t* base = a.c.k_codes + codes_at<DH>(a.c, max(page, 0), g) + (size_t)place * DH + lg * 16;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+      for (int blk = 0; blk < NB; ++blk) kf[c][blk] = *reinterpret_cast<const uint4*>(base + c * DH + blk * 64);
+    const size_t at = scales_at<DH>(a.c, max(page, 0), g) + place;
+#pragma unroll
+    for (int blk = 0; blk < NB; ++blk) ks[blk] = scales4<S16>(a.c.k_scales, at + ((size_t)blk << a.c.page_shift));
+  };
+  auto load_values = [&](int tile, int page, int k_page) {
+    const int place = min(tile * kTile + 16 * lg, last_v) & P1;
+    const int8_t* base = a.c.v_codes + codes_at<DH>(a.c, max(page, 0), g) + ((size_t)n << a.c.page_shift) + place;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) vf[d] = *reinterpret_cast<const uint4*>(base + ((size_t)d << (a.c.page_shift + 4)));
+    const size_t at = scales_at<DH>(a.c, max(k_page, 0), g) + (min(tile * kTile + 4 * n, last_k) & P1);
+#pragma unroll
+    for (int blk = 0; blk < NB; ++blk) vs[blk] = scales4<S16>(a.c.v_scales, at + ((size_t)blk << a.c.page_shift));
+  };
+
+  int tile = first + wave;
+  int pk = -1, pk_next = -1, pv_next = -1;
+  if (tile < end) {
+    pk = page_k(tile);
+    const int pv = page_v(tile);
+    load_keys(tile, pk);
+    load_values(tile, pv, pk);
+    if (tile + kWaves < end) { pk_next = page_k(tile + kWaves); pv_next = page_v(tile + kWaves); }
+  }
+  for (; tile < end; tile += kWaves) {
+    const bool more = tile + kWaves < end;
+    // ---- scores
+    float p[RT][4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) p[rt][c] = 0.f;
+#pragma unroll
+      for (int blk = 0; blk < NB; ++blk) {
+        const float k = c == 0 ? ks[blk].x : c == 1 ? ks[blk].y : c == 2 ? ks[blk].z : ks[blk].w;
+        const i32x4 kv = __builtin_bit_cast(i32x4, kf[c][blk]);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+          const i32x4 acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(qf[rt][blk], kv, i32x4{0, 0, 0, 0}, 0, 0, 0);
+          p[rt][c] = fmaf(joined<BYTES>(acc), k * qs[rt][blk], p[rt][c]);
+        }
+      }
+    }
+    const int pk_now = pk;
+    if (more) {
+      pk = pk_next;
+      load_keys(tile + kWaves, pk);
+    }
+    // ---- which of them count; the values' scales of what does not may be anything
+    const int j0 = tile * kTile;
+    const bool inner = j0 + kTile <= s.past && __ballot(pk_now < 0) == 0;
+    float vn[NB][4];
+#pragma unroll
+    for (int blk = 0; blk < NB; ++blk) { vn[blk][0] = vs[blk].x; vn[blk][1] = vs[blk].y; vn[blk][2] = vs[blk].z; vn[blk][3] = vs[blk].w; }
+    if (!inner) {
+      bool any[4] = {false, false, false, false};
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const int j = j0 + 4 * n + c, u = j - s.past;
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+          const bool sees = pk_now >= 0 && (u < 0 || (u < s.fresh && (a.tree ? (see[rt] >> u) & 1 : u <= my_t[rt])));
+          if (!sees) p[rt][c] = -INFINITY;
+          any[c] |= sees;
+        }
+        // a token that this lane's rows do not see may be seen by the other lane groups' rows
+        any[c] |= __shfl_xor((int)any[c], 16, 64) != 0;
+        any[c] |= __shfl_xor((int)any[c], 32, 64) != 0;
+#pragma unroll
+        for (int blk = 0; blk < NB; ++blk) vn[blk][c] = any[c] ? vn[blk][c] : 0.f;
+      }
+    }
+    // ---- the values' scales relative to a power of two that is above them all
+    float back[NB];
+#pragma unroll
+    for (int blk = 0; blk < NB; ++blk) {
+      auto largest = [&] {             // none is negative, so they compare as whole numbers; what is no number comes out on top
+        return umax16(max(max(__float_as_uint(vn[blk][0]), __float_as_uint(vn[blk][1])),
+                          max(__float_as_uint(vn[blk][2]), __float_as_uint(vn[blk][3]))));
+      };
+      uint32_t top = largest();
+      if (__ballot(top >= 0x7F800000u)) {      // an infinite value or none: for the rows that see it, and no others
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          if (__float_as_uint(vn[blk][c]) < 0x7F800000u) continue;
+          vn[blk][c] = 0.f;
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt)
+            if (p[rt][c] != -INFINITY) l[rt] = __uint_as_float(0x7FC00000u);
+        }
+        top = largest();
+      }
+      const int ex = (int)(top >> 23) - 126;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) vn[blk][c] = ldexpf(vn[blk][c], BITS - ex);
+      back[blk] = ldexpf(1.0f, ex - BITS);
+    }
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      // ---- softmax of this tile
+      const float mn = max16(fmaxf(fmaxf(m[rt], fmaxf(p[rt][0], p[rt][1])), fmaxf(p[rt][2], p[rt][3])));
+      const float top = mn == -INFINITY ? 0.f : mn;
+      const float keep = __builtin_amdgcn_exp2f(m[rt] - top);
+      m[rt] = mn;
+      l[rt] *= keep;
+      uint32_t w[NB][4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const float x = __builtin_amdgcn_exp2f(p[rt][c] - top);
+        l[rt] += x;
+#pragma unroll
+        for (int blk = 0; blk < NB; ++blk) w[blk][c] = digits<BYTES>((int)rintf(x * vn[blk][c]));
+      }
+      // ---- byte i of four tokens to a word of row 4 q + i
+#pragma unroll
+      for (int blk = 0; blk < NB; ++blk) {
+        const uint32_t a0 = __builtin_amdgcn_perm(w[blk][1], w[blk][0], 0x05010400u), a1 = __builtin_amdgcn_perm(w[blk][3], w[blk][2], 0x05010400u);
+        const uint32_t b0 = __builtin_amdgcn_perm(w[blk][1], w[blk][0], 0x07030602u), b1 = __builtin_amdgcn_perm(w[blk][3], w[blk][2], 0x07030602u);
+        uint32_t* to = weights + blk * 16 * kRowPitch + lg * 4 * kRowPitch + n;
+        to[0] = __builtin_amdgcn_perm(a1, a0, 0x05040100u);
+        to[kRowPitch] = __builtin_amdgcn_perm(a1, a0, 0x07060302u);
+        to[2 * kRowPitch] = __builtin_amdgcn_perm(b1, b0, 0x05040100u);
+        to[3 * kRowPitch] = __builtin_amdgcn_perm(b1, b0, 0x07060302u);
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      i32x4 pf[NB];
+#pragma unroll
+      for (int blk = 0; blk < NB; ++blk)
+        pf[blk] = *reinterpret_cast<const i32x4*>(weights + blk * 16 * kRowPitch + n * kRowPitch + lg * 4);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        const i32x4 acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(pf[d / 4], __builtin_bit_cast(i32x4, vf[d]), i32x4{0, 0, 0, 0}, 0, 0, 0);
+        o[rt][d] = fmaf(o[rt][d], keep, joined<BYTES>(acc) * back[d / 4]);
+      }
+    }
+    if (more) {
+      load_values(tile + kWaves, pv_next, pk);
+      if (tile + 2 * kWaves < end) { pk_next = page_k(tile + 2 * kWaves); pv_next = page_v(tile + 2 * kWaves); }
+    }
+  }
+
+  // ---- the wavefronts' results, one after the other in a fixed order
+  __syncthreads();
+  float* ow = reinterpret_cast<float*>(lds);                  // [wave][row][d_head]
+  float* ml = ow + kWaves * Q * DH;                           // [wave][row][2]
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const float total = sum16(l[rt]);
+    const int q = wave * Q + rt * 4 + lg;
+    if (n == 0) { ml[2 * q] = m[rt]; ml[2 * q + 1] = total; }
+#pragma unroll
+    for (int d = 0; d < DT; ++d) ow[q * DH + d * 16 + n] = o[rt][d];
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < Q * DH; i += kThreads) {
+    const int q = i / DH, d = i - q * DH, r = r0 + q;
+    if (r >= rows) continue;
+    float mw[kWaves], top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) { mw[w] = ml[2 * (w * Q + q)]; top = fmaxf(top, mw[w]); }
+    const float ref = top == -INFINITY ? 0.f : top;
+    float total = 0.f, x = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float f = __builtin_amdgcn_exp2f(mw[w] - ref);
+      total = fmaf(ml[2 * (w * Q + q) + 1], f, total);
+      x = fmaf(ow[(w * Q + q) * DH + d], f, x);
+    }
+    if (a.splits == 1) {
+      Elem<T>::store(reinterpret_cast<T*>(a.out) + ((size_t)b * a.c.tokens + r / a.group) * a.out_pitch +
+                     (size_t)(g * a.group + r % a.group) * DH + d, total == 0.f ? 0.f : x / total);
+    } else {
+      const size_t at = (size_t)blockIdx.x * Q + q;
+      a.part_o[at * DH + d] = x;
+      if (d == 0) { a.part_ml[2 * at] = top; a.part_ml[2 * at + 1] = total; }
+    }
+  }
+}
+
+// The splits of one row group's rows joined: partial results in the order of the splits.
+template <typename T, int DH>
+__global__ __launch_bounds__(kThreads) void cache_attention_join_kernel(AttnArgs a, int Q) {
+  int unit = blockIdx.x;
+  const int g = unit % a.c.KV; unit /= a.c.KV;
+  const int rg = unit % a.row_groups, b = unit / a.row_groups;
+  const Span s = span_of(a.c, b);
+  const int r0 = rg * Q, rows = s.fresh * a.group;
+  for (int i = threadIdx.x; i < Q * DH; i += kThreads) {
+    const int q = i / DH, d = i - q * DH, r = r0 + q;
+    if (r >= rows) return;
+    const size_t at = (size_t)blockIdx.x * a.splits * Q + q;
+    float top = -INFINITY;
+    for (int p = 0; p < a.splits; ++p) top = fmaxf(top, a.part_ml[2 * (at + (size_t)p * Q)]);
+    const float ref = top == -INFINITY ? 0.f : top;
+    float total = 0.f, x = 0.f;
+    for (int p = 0; p < a.splits; ++p) {
+      const size_t k = at + (size_t)p * Q;
+      const float f = __builtin_amdgcn_exp2f(a.part_ml[2 * k] - ref);
+      total = fmaf(a.part_ml[2 * k + 1], f, total);
+      x = fmaf(a.part_o[k * DH + d], f, x);
+    }
+    Elem<T>::store(reinterpret_cast<T*>(a.out) + ((size_t)b * a.c.tokens + r / a.group) * a.out_pitch +
+                   (size_t)(g * a.group + r % a.group) * DH + d, total == 0.f ? 0.f : x / total);
+  }
+}
+
+// How the rows and the tokens of a call are cut.
+struct Cut {
+  int row_tiles;       // RT: tiles of four rows per workgroup
+  int row_groups, splits, chunk;
+};
+Cut cut_of(const swarm_cache_config* c, int tokens, int max_len) {
+  Cut k{};
+  const int rows = tokens * (c->n_heads / c->n_kv_heads);
+  k.row_tiles = rows <= 4 ? 1 : rows <= 8 ? 2 : 4;
+  k.row_groups = (rows + 4 * k.row_tiles - 1) / (4 * k.row_tiles);
+  const long long cap = (long long)c->table_pages * c->page_tokens;
+  const long long len = max_len > 0 ? std::min<long long>(max_len, cap) : cap;
+  const long long tiles = (len + kTile - 1) / kTile, whole = (long long)c->batch * c->n_kv_heads * k.row_groups;
+  // about 2048 workgroups, eight for every compute unit, each of four tiles at least (one for every wavefront)
+  const long long chunk = std::max(4ll, std::min<long long>(1ll << 24, (whole * tiles + 2047) / 2048));
+  k.splits = (int)std::max(1ll, (tiles + chunk - 1) / chunk);
+  k.chunk = (int)chunk;
+  return k;
 }
 
 }  // namespace
 
-size_t cache_attention_scratch_bytes(const swarm_cache_config*, int, int) { return 0; }
+size_t cache_attention_scratch_bytes(const swarm_cache_config* c, int tokens, int max_len) {
+  const Cut k = cut_of(c, tokens, max_len);
+  if (k.splits == 1) return 0;
+  const size_t rows = (size_t)c->batch * c->n_kv_heads * k.row_groups * k.splits * 4 * k.row_tiles;
+  return ((rows * (c->d_head + 2) * 4) + 255) & ~(size_t)255;
+}
 
-swarm_status cache_attention_launch(const swarm_cache_config* c, const CacheArgs& args, int, const void* q, size_t q_pitch,
-                                    const uint64_t* tree, void* out, size_t out_pitch, void*, hipStream_t st) {
-  const AttnArgs a{args, q, out, tree, q_pitch, out_pitch, c->scale_bits == 16};
-  const long long blocks = (long long)c->batch * args.tokens * c->n_heads;
-  if (blocks > 0x7FFFFFFF) return SWARM_ERR_SHAPE;
-  const dim3 grid((unsigned)blocks), block(64);
-  if (c->dtype == SWARM_BF16) {
-    if (c->d_head == 64) hipLaunchKernelGGL((cache_attention_kernel<bf16_raw, 64>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((cache_attention_kernel<bf16_raw, 128>), grid, block, 0, st, a);
-  } else {
-    if (c->d_head == 64) hipLaunchKernelGGL((cache_attention_kernel<float, 64>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((cache_attention_kernel<float, 128>), grid, block, 0, st, a);
-  }
+namespace {
+template <typename T, int DH>
+swarm_status launch_bytes(const AttnArgs& a, const Cut& k, hipStream_t st) {
+  const long long whole = (long long)a.c.B * a.c.KV * k.row_groups;
+  if (whole * k.splits > 0x7FFFFFFF) return SWARM_ERR_SHAPE;
+  const dim3 grid((unsigned)(whole * k.splits)), block(kThreads);
+#define SWARM_ATTN(RT)                                                                                                          \
+  do {                                                                                                                          \
+    if (a.s16) hipLaunchKernelGGL((cache_attention_bytes_kernel<T, DH, RT, true>), grid, block, 0, st, a);                      \
+    else hipLaunchKernelGGL((cache_attention_bytes_kernel<T, DH, RT, false>), grid, block, 0, st, a);                           \
+  } while (0)
+  if (k.row_tiles == 1) SWARM_ATTN(1);
+  else if (k.row_tiles == 2) SWARM_ATTN(2);
+  else SWARM_ATTN(4);
+#undef SWARM_ATTN
+  if (k.splits > 1)
+    hipLaunchKernelGGL((cache_attention_join_kernel<T, DH>), dim3((unsigned)whole), block, 0, st, a, 4 * k.row_tiles);
   return launch_status();
+}
+}  // namespace
+
+swarm_status cache_attention_launch(const swarm_cache_config* c, const CacheArgs& args, int max_len, const void* q, size_t q_pitch,
+                                    const uint64_t* tree, void* out, size_t out_pitch, void* scratch, hipStream_t st) {
+  const Cut k = cut_of(c, args.tokens, max_len);
+  AttnArgs a{args, q, out, tree, q_pitch, out_pitch, nullptr, nullptr, c->n_heads / c->n_kv_heads, k.row_groups, k.splits, k.chunk,
+             c->scale_bits == 16};
+  if (k.splits > 1) {
+    const size_t rows = (size_t)c->batch * c->n_kv_heads * k.row_groups * k.splits * 4 * k.row_tiles;
+    a.part_o = (float*)scratch;
+    a.part_ml = a.part_o + rows * c->d_head;
+  }
+  if (c->dtype == SWARM_BF16) return c->d_head == 64 ? launch_bytes<bf16_raw, 64>(a, k, st) : launch_bytes<bf16_raw, 128>(a, k, st);
+  return c->d_head == 64 ? launch_bytes<float, 64>(a, k, st) : launch_bytes<float, 128>(a, k, st);
 }
 
 }  // namespace swarm
