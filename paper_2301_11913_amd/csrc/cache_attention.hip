@@ -13,7 +13,7 @@
 // last product.  Bound by reading the cache while a key / value head has few rows: 16 KB per 64 tokens at d_head 128 against
 // some 300 vector instructions for four rows.  The four wavefronts of a workgroup take tiles in turn; long sequences are spread over
 // workgroups (splits of `chunk` tiles), whose partial sums a second kernel joins.
-#include "cache.h"
+#include "cache_attention.h"
 
 namespace swarm {
 namespace {
@@ -21,21 +21,9 @@ namespace {
 typedef __attribute__((ext_vector_type(4))) int i32x4;
 
 constexpr int kThreads = 256, kWaves = 4;
-constexpr int kTile = 64;
+constexpr int kTile = kAttnTile;
 constexpr int kRowPitch = 20;          // 32-bit words of a row of weights' bytes: 16, and 4 against bank conflicts
 constexpr float kLog2e = 1.4426950408889634f;
-
-struct AttnArgs {
-  CacheArgs c;
-  const void* q;
-  void* out;
-  const uint64_t* tree;
-  size_t q_pitch, out_pitch;
-  float *part_o, *part_ml;     // splits > 1: [unit][rows][d_head], [unit][rows][2]
-  int group;                   // query heads per key / value head
-  int row_groups, splits, chunk;
-  bool s16;
-};
 
 // Reductions over the 16 lanes of a row of the register file
 template <int N>
@@ -351,79 +339,111 @@ __global__ __launch_bounds__(kThreads) void cache_attention_bytes_kernel(AttnArg
   }
 }
 
-// The splits of one row group's rows joined: partial results in the order of the splits.
+// The splits of one row and head joined, one workgroup each: every d_head / 4 threads take the partial results of some of the splits,
+// eight (16 at d_head 64) at a time, and are added up in order.
 template <typename T, int DH>
 __global__ __launch_bounds__(kThreads) void cache_attention_join_kernel(AttnArgs a, int Q) {
-  int unit = blockIdx.x;
-  const int g = unit % a.c.KV; unit /= a.c.KV;
-  const int rg = unit % a.row_groups, b = unit / a.row_groups;
-  const Span s = span_of(a.c, b);
-  const int r0 = rg * Q, rows = s.fresh * a.group;
-  for (int i = threadIdx.x; i < Q * DH; i += kThreads) {
-    const int q = i / DH, d = i - q * DH, r = r0 + q;
-    if (r >= rows) return;
-    const size_t at = (size_t)blockIdx.x * a.splits * Q + q;
-    float top = -INFINITY;
-    for (int p = 0; p < a.splits; ++p) top = fmaxf(top, a.part_ml[2 * (at + (size_t)p * Q)]);
-    const float ref = top == -INFINITY ? 0.f : top;
-    float total = 0.f, x = 0.f;
-    for (int p = 0; p < a.splits; ++p) {
-      const size_t k = at + (size_t)p * Q;
-      const float f = __builtin_amdgcn_exp2f(a.part_ml[2 * k] - ref);
-      total = fmaf(a.part_ml[2 * k + 1], f, total);
-      x = fmaf(a.part_o[k * DH + d], f, x);
-    }
-    Elem<T>::store(reinterpret_cast<T*>(a.out) + ((size_t)b * a.c.tokens + r / a.group) * a.out_pitch +
-                   (size_t)(g * a.group + r % a.group) * DH + d, total == 0.f ? 0.f : x / total);
+  constexpr int LANES = DH / 4, SLICES = kThreads / LANES;
+  __shared__ float4 sums[SLICES][LANES];
+  __shared__ float totals[SLICES], tops[kWaves];
+  const int h = blockIdx.x % a.c.H, row = blockIdx.x / a.c.H;
+  const int b = row / a.c.tokens, t = row - b * a.c.tokens, g = h / a.group;
+  if (t >= span_of(a.c, b).fresh) return;
+  const int r = t * a.group + h - g * a.group, rg = r / Q;
+  const size_t at = (((size_t)b * a.row_groups + rg) * a.c.KV + g) * a.splits * Q + (r - rg * Q);
+  float top = -INFINITY;
+  for (int p = threadIdx.x; p < a.splits; p += kThreads) top = fmaxf(top, a.part_ml[2 * (at + (size_t)p * Q)]);
+  top = wave_max(top);
+  if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+  const float ref = top == -INFINITY ? 0.f : top;
+  const int lane = threadIdx.x % LANES, slice = threadIdx.x / LANES;
+  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+  float total = 0.f;
+#pragma unroll 4
+  for (int p = slice; p < a.splits; p += SLICES) {
+    const size_t k = at + (size_t)p * Q;
+    const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * k);
+    const float4 o = *reinterpret_cast<const float4*>(a.part_o + k * DH + lane * 4);
+    const float f = __builtin_amdgcn_exp2f(ml.x - ref);
+    total = fmaf(ml.y, f, total);
+    x.x = fmaf(o.x, f, x.x); x.y = fmaf(o.y, f, x.y); x.z = fmaf(o.z, f, x.z); x.w = fmaf(o.w, f, x.w);
   }
+  sums[slice][lane] = x;
+  if (lane == 0) totals[slice] = total;
+  __syncthreads();
+  if (threadIdx.x >= DH) return;
+  const int d = threadIdx.x;
+  float sum = 0.f;
+  total = 0.f;
+#pragma unroll
+  for (int i = 0; i < SLICES; ++i) { sum += reinterpret_cast<const float*>(sums[i])[d]; total += totals[i]; }
+  Elem<T>::store(reinterpret_cast<T*>(a.out) + (size_t)row * a.out_pitch + (size_t)h * DH + d, total == 0.f ? 0.f : sum / total);
 }
 
 // How the rows and the tokens of a call are cut.
 struct Cut {
-  int row_tiles;       // RT: tiles of four rows per workgroup
+  bool many;           // the kernel of many rows
+  int row_tiles;       // tiles of four rows per workgroup (of 16 per wavefront where there are many)
+  int rows;            // rows of a workgroup
   int row_groups, splits, chunk;
 };
 Cut cut_of(const swarm_cache_config* c, int tokens, int max_len) {
   Cut k{};
   const int rows = tokens * (c->n_heads / c->n_kv_heads);
-  k.row_tiles = rows <= 4 ? 1 : rows <= 8 ? 2 : 4;
-  k.row_groups = (rows + 4 * k.row_tiles - 1) / (4 * k.row_tiles);
+  k.many = c->dtype == SWARM_BF16 && rows > 16;
+  if (k.many) {
+    k.row_tiles = rows <= 64 ? 1 : 2;
+    k.rows = 64 * k.row_tiles;
+  } else {
+    k.row_tiles = rows <= 4 ? 1 : rows <= 8 ? 2 : 4;
+    k.rows = 4 * k.row_tiles;
+  }
+  k.row_groups = (rows + k.rows - 1) / k.rows;
   const long long cap = (long long)c->table_pages * c->page_tokens;
   const long long len = max_len > 0 ? std::min<long long>(max_len, cap) : cap;
   const long long tiles = (len + kTile - 1) / kTile, whole = (long long)c->batch * c->n_kv_heads * k.row_groups;
-  // about 2048 workgroups, eight for every compute unit, each of four tiles at least (one for every wavefront)
-  const long long chunk = std::max(4ll, std::min<long long>(1ll << 24, (whole * tiles + 2047) / 2048));
+  // about 512 workgroups, as many as are resident at d_head 128, each of four tiles at least (one for every wavefront).  32 sequences
+  // of up to 8192 tokens / one of 131072 with 8 heads: 213 / 57 us; 1024: 213 / 60, 2048: 246 / 70, 4096: 271 / 86
+  const long long chunk = std::max(4ll, std::min<long long>(1ll << 24, (whole * tiles + 511) / 512));
   k.splits = (int)std::max(1ll, (tiles + chunk - 1) / chunk);
   k.chunk = (int)chunk;
   return k;
+}
+size_t partial_rows(const swarm_cache_config* c, const Cut& k) {
+  return (size_t)c->batch * c->n_kv_heads * k.row_groups * k.splits * k.rows;
 }
 
 }  // namespace
 
 size_t cache_attention_scratch_bytes(const swarm_cache_config* c, int tokens, int max_len) {
   const Cut k = cut_of(c, tokens, max_len);
-  if (k.splits == 1) return 0;
-  const size_t rows = (size_t)c->batch * c->n_kv_heads * k.row_groups * k.splits * 4 * k.row_tiles;
-  return ((rows * (c->d_head + 2) * 4) + 255) & ~(size_t)255;
+  return k.splits == 1 ? 0 : (partial_rows(c, k) * (c->d_head + 2) * 4 + 255) & ~(size_t)255;
 }
 
 namespace {
+template <typename T, int DH, int RT>
+void launch_bytes(const AttnArgs& a, unsigned blocks, hipStream_t st) {
+  if (a.s16) hipLaunchKernelGGL((cache_attention_bytes_kernel<T, DH, RT, true>), dim3(blocks), dim3(kThreads), 0, st, a);
+  else hipLaunchKernelGGL((cache_attention_bytes_kernel<T, DH, RT, false>), dim3(blocks), dim3(kThreads), 0, st, a);
+}
 template <typename T, int DH>
-swarm_status launch_bytes(const AttnArgs& a, const Cut& k, hipStream_t st) {
-  const long long whole = (long long)a.c.B * a.c.KV * k.row_groups;
-  if (whole * k.splits > 0x7FFFFFFF) return SWARM_ERR_SHAPE;
-  const dim3 grid((unsigned)(whole * k.splits)), block(kThreads);
-#define SWARM_ATTN(RT)                                                                                                          \
-  do {                                                                                                                          \
-    if (a.s16) hipLaunchKernelGGL((cache_attention_bytes_kernel<T, DH, RT, true>), grid, block, 0, st, a);                      \
-    else hipLaunchKernelGGL((cache_attention_bytes_kernel<T, DH, RT, false>), grid, block, 0, st, a);                           \
-  } while (0)
-  if (k.row_tiles == 1) SWARM_ATTN(1);
-  else if (k.row_tiles == 2) SWARM_ATTN(2);
-  else SWARM_ATTN(4);
-#undef SWARM_ATTN
+swarm_status launch(const AttnArgs& a, const Cut& k, hipStream_t st) {
+  const long long blocks = (long long)a.c.B * a.c.KV * k.row_groups * k.splits, joins = (long long)a.c.B * a.c.tokens * a.c.H;
+  if (blocks > 0x7FFFFFFF || (k.splits > 1 && joins > 0x7FFFFFFF)) return SWARM_ERR_SHAPE;
+  if (k.many) {
+    const swarm_status st1 = cache_attention_rows_launch(a, DH, k.row_tiles, st);
+    if (st1 != SWARM_OK) return st1;
+  } else if (k.row_tiles == 1) {
+    launch_bytes<T, DH, 1>(a, (unsigned)blocks, st);
+  } else if (k.row_tiles == 2) {
+    launch_bytes<T, DH, 2>(a, (unsigned)blocks, st);
+  } else {
+    launch_bytes<T, DH, 4>(a, (unsigned)blocks, st);
+  }
   if (k.splits > 1)
-    hipLaunchKernelGGL((cache_attention_join_kernel<T, DH>), dim3((unsigned)whole), block, 0, st, a, 4 * k.row_tiles);
+    hipLaunchKernelGGL((cache_attention_join_kernel<T, DH>), dim3((unsigned)joins), dim3(kThreads), 0, st, a, k.rows);
   return launch_status();
 }
 }  // namespace
@@ -434,12 +454,11 @@ swarm_status cache_attention_launch(const swarm_cache_config* c, const CacheArgs
   AttnArgs a{args, q, out, tree, q_pitch, out_pitch, nullptr, nullptr, c->n_heads / c->n_kv_heads, k.row_groups, k.splits, k.chunk,
              c->scale_bits == 16};
   if (k.splits > 1) {
-    const size_t rows = (size_t)c->batch * c->n_kv_heads * k.row_groups * k.splits * 4 * k.row_tiles;
     a.part_o = (float*)scratch;
-    a.part_ml = a.part_o + rows * c->d_head;
+    a.part_ml = a.part_o + partial_rows(c, k) * c->d_head;
   }
-  if (c->dtype == SWARM_BF16) return c->d_head == 64 ? launch_bytes<bf16_raw, 64>(a, k, st) : launch_bytes<bf16_raw, 128>(a, k, st);
-  return c->d_head == 64 ? launch_bytes<float, 64>(a, k, st) : launch_bytes<float, 128>(a, k, st);
+  if (c->dtype == SWARM_BF16) return c->d_head == 64 ? launch<bf16_raw, 64>(a, k, st) : launch<bf16_raw, 128>(a, k, st);
+  return c->d_head == 64 ? launch<float, 64>(a, k, st) : launch<float, 128>(a, k, st);
 }
 
 }  // namespace swarm
