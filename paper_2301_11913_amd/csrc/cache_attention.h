@@ -18,7 +18,7 @@ struct AttnArgs {
   bool s16;
 };
 
-// bf16, many rows: 16 * tiles rows per wavefront, tiles 1 or 2 (cache_attention_rows.hip)
-swarm_status cache_attention_rows_launch(const AttnArgs& a, int dh, int tiles, hipStream_t st);
+// bf16, many rows: 32 * row_waves rows per workgroup, row_waves 2 or 4 (cache_attention_rows.hip)
+swarm_status cache_attention_rows_launch(const AttnArgs& a, int dh, int row_waves, hipStream_t st);
 
 }  // namespace swarm

@@ -385,7 +385,7 @@ __global__ __launch_bounds__(kThreads) void cache_attention_join_kernel(AttnArgs
 // How the rows and the tokens of a call are cut.
 struct Cut {
   bool many;           // the kernel of many rows
-  int row_tiles;       // tiles of four rows per workgroup (of 16 per wavefront where there are many)
+  int row_tiles;       // tiles of four rows per workgroup (of 32 where there are many)
   int rows;            // rows of a workgroup
   int row_groups, splits, chunk;
 };
@@ -394,8 +394,8 @@ Cut cut_of(const swarm_cache_config* c, int tokens, int max_len) {
   const int rows = tokens * (c->n_heads / c->n_kv_heads);
   k.many = c->dtype == SWARM_BF16 && rows > 16;
   if (k.many) {
-    k.row_tiles = rows <= 64 ? 1 : 2;
-    k.rows = 64 * k.row_tiles;
+    k.row_tiles = rows <= 64 ? 2 : 4;
+    k.rows = 32 * k.row_tiles;
   } else {
     k.row_tiles = rows <= 4 ? 1 : rows <= 8 ? 2 : 4;
     k.rows = 4 * k.row_tiles;

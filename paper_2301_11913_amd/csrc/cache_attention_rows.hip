@@ -1,15 +1,18 @@
 // Attention of many new tokens over the paged int8 cache, bf16: drafted trees, prompts.
 //
 // The codes are whole numbers of 8 bits, which bf16 holds exactly: a tile of 64 tokens is read once per workgroup, turned into bf16 on
-// the way into LDS (one conversion per code, one byte permutation per two) and contracted with the queries on v_mfma_f32_16x16x32_bf16.  The
-// scales never touch the codes: a score is the sum over the blocks of 64 elements of (products) * (key's scale), and the weight of a
+// the way into LDS (one conversion per code, one byte permutation per two) and contracted with the queries on v_mfma_f32_32x32x16_bf16.
+// The scales never touch the codes: a score is the sum over the blocks of 64 elements of (products) * (key's scale), and the weight of a
 // value is p_j times its scale, so the only roundings beyond fp32 are those of the weights to bf16.
-//   scores  S^T [token][query] = K Q^T: a lane owns one query column, so maximum and sum need no more than two exchanges between lanes;
-//           row 4 a + i of key tile (h, u) is token 32 h + 8 a + 4 u + i, which leaves a lane eight consecutive tokens' weights:
+//   scores  S^T [token][query] = K Q^T, 32 tokens x 32 queries: a lane owns one query column, so a maximum or a sum needs one exchange
+//           between lanes; row 8 a + 4 b + i of the keys' operand is token 16 (a / 2) + 8 b + 4 (a % 2) + i, which leaves a lane eight
+//           consecutive tokens' weights twice:
 //   output  O^T [element][query] = V^T P^T takes them as its operand without an exchange, and the transposed values of the cache are
 //           V^T as it lies.
-// The running maximum is raised only when a score passes it by 2^8.  LDS holds two stages; chunks of 16 bytes are XOR-swizzled so that a
-// fragment's 16 rows fall on different banks.
+// RW wavefronts of a workgroup take 32 rows each; with KW = 2 two wavefronts share rows and take 32 of a tile's 64 tokens each
+// (few rows, where the tile's conversion and the wait for it would outweigh them), joined at the end.
+// The running maximum is raised only when a score passes it by 2^8.  LDS holds two stages; 16-byte chunks are XOR-swizzled so that the 16
+// rows of a fragment that are read together fall on different banks.
 #include "cache_attention.h"
 
 namespace swarm {
@@ -18,9 +21,8 @@ namespace {
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(2))) float f32x2;
-typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(16))) float f32x16;
 
-constexpr int kThreads = 256, kWaves = 4;
 constexpr float kLog2e = 1.4426950408889634f;
 
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
@@ -34,30 +36,29 @@ __device__ __forceinline__ uint2 codes4(uint32_t w) {
   return make_uint2(__builtin_amdgcn_perm(b, a, 0x07060302u), __builtin_amdgcn_perm(d, c, 0x07060302u));
 }
 
-template <int DH> struct Tiles {
-  static constexpr int NB = DH / 64;
-  static constexpr int KCH = DH / 8;                       // 16-byte chunks of a key row
-  static constexpr int PIECES = 64 * DH / 16 / kThreads;   // pieces of 16 codes per thread, of keys and of values
-  struct Stage {
-    uint4 k[64 * KCH];
-    uint4 v[DH * 8];
-    float ks[NB][64], vs[NB][64];                          // keys' with the factor of the scores in them
-  };
+template <int DH> struct Stage {
+  static constexpr int NB = DH / 64, CH = DH / 8;          // 16-byte chunks of a key row
+  uint4 k[64 * CH];
+  uint4 v[DH * 8];
+  float ks[NB][64], vs[NB][64];                            // keys' with the factor of the scores in them
   static __device__ __forceinline__ int k_at(int key, int chunk) {
-    if constexpr (DH == 128) return key * KCH + (chunk ^ (((key >> 1) & 12) | (key & 3)));
-    return key * KCH + (chunk ^ (((key >> 1) & 4) | (key & 3)));
+    return key * CH + (chunk ^ (DH == 128 ? key & 15 : (key >> 1) & 7));
   }
-  static __device__ __forceinline__ int v_at(int d, int chunk) { return d * 8 + (chunk ^ (d & 7)); }
+  static __device__ __forceinline__ int v_at(int d, int chunk) { return d * 8 + (chunk ^ ((d >> 1) & 7)); }
 };
 
-template <int DH, int NQ, bool S16>
-__global__ __launch_bounds__(kThreads, 2) void cache_attention_rows_kernel(AttnArgs a) {
-  using T = Tiles<DH>;
-  constexpr int NB = T::NB, DT = DH / 16, KK = DH / 32, Q = kWaves * 16 * NQ;
+template <int DH, int RW, int KW, bool S16>
+__global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(AttnArgs a) {
+  using St = Stage<DH>;
+  constexpr int THREADS = 64 * RW * KW;
+  constexpr int NB = DH / 64, DT = DH / 32, KK = DH / 16, Q = 32 * RW;
+  constexpr int PIECES = 64 * DH / 16 / THREADS;           // pieces of 16 codes per thread, of keys and of values
+  constexpr int SCALES = 2 * NB * 64, SC = (SCALES + THREADS - 1) / THREADS;
   extern __shared__ __attribute__((aligned(16))) char lds[];
-  typename T::Stage* stage = reinterpret_cast<typename T::Stage*>(lds);
-  const int lane = threadIdx.x & 63, n = lane & 15, lg = lane >> 4;
+  St* stage = reinterpret_cast<St*>(lds);
+  const int lane = threadIdx.x & 63, n = lane & 31, lh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row_wave = wave % RW, key_wave = wave / RW;
   // workgroups go to the 8 XCDs in turn: all units of a sequence and head to one, which keeps its tiles in that XCD's L2; the last
   // rows, which see the most, first
   const int per_pair = a.row_groups * a.splits, x = blockIdx.x >> 3;
@@ -73,50 +74,48 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attention_rows_kernel(AttnA
   const int first = split * a.chunk, end = split + 1 == a.splits ? tiles : min(tiles, first + a.chunk);
 
   // ---- this wavefront's queries, and up to where each sees
-  bf16x8 qf[NQ][KK];
-  uint64_t among[NQ];                    // which of the new tokens (tree)
-  int limit[NQ];                         // tokens below it are seen (the past; without a tree the row's own too)
-  const int w0 = r0 + wave * 16 * NQ;
+  const int w0 = r0 + row_wave * 32, r = w0 + n;
+  const bool real = r < rows;
+  const int t = real ? r / a.group : 0, head = g * a.group + (real ? r - t * a.group : 0);
+  const size_t row = (size_t)b * a.c.tokens + t;
+  bf16x8 qf[KK];
+  {
+    const bf16_raw* src = reinterpret_cast<const bf16_raw*>(a.q) + row * a.q_pitch + (size_t)head * DH + lh * 8;
 #pragma unroll
-  for (int q = 0; q < NQ; ++q) {
-    const int r = w0 + q * 16 + n;
-    const bool real = r < rows;
-    const int t = real ? r / a.group : 0, h = real ? r - t * a.group : 0;
-    const bf16_raw* src = reinterpret_cast<const bf16_raw*>(a.q) + ((size_t)b * a.c.tokens + t) * a.q_pitch + (size_t)(g * a.group + h) * DH;
-#pragma unroll
-    for (int k = 0; k < KK; ++k) {
-      const uint4 v = real ? *reinterpret_cast<const uint4*>(src + k * 32 + lg * 8) : make_uint4(0, 0, 0, 0);
-      qf[q][k] = __builtin_bit_cast(bf16x8, v);
-    }
-    among[q] = 0;
-    if (a.tree && real) among[q] = a.tree[(size_t)b * a.c.tokens + t] & (s.fresh >= 64 ? ~0ull : (1ull << s.fresh) - 1);
-    limit[q] = a.tree ? s.past : s.past + t + 1;
+    for (int k = 0; k < KK; ++k)
+      qf[k] = __builtin_bit_cast(bf16x8, real ? *reinterpret_cast<const uint4*>(src + k * 16) : make_uint4(0, 0, 0, 0));
   }
-  // tiles below `inner` are seen whole by all rows; without a tree, tiles from `outer` on by none of this wavefront's
+  // which of the new tokens it sees (tree), and the tokens below `limit` (the past; without a tree up to the row's own)
+  const uint64_t among = a.tree && real ? a.tree[row] & (s.fresh >= 64 ? ~0ull : (1ull << s.fresh) - 1) : 0;
+  const int limit = a.tree ? s.past : s.past + t + 1;
+  // tokens below `inner` are seen by all rows of this wavefront; from `outer` on by none
   const int inner = a.tree ? s.past : s.past + min(w0, rows - 1) / a.group + 1;
-  const int outer = w0 >= rows ? 0 : a.tree ? len : s.past + (min(w0 + 16 * NQ, rows) - 1) / a.group + 1;
+  const int outer = w0 >= rows ? 0 : a.tree ? len : s.past + (min(w0 + 32, rows) - 1) / a.group + 1;
 
-  f32x4 o[NQ][DT];
-  float m[NQ], l[NQ];
+  f32x16 o[DT];
+  float m = -INFINITY, l = 0.f;
 #pragma unroll
-  for (int q = 0; q < NQ; ++q) {
-    m[q] = -INFINITY; l[q] = 0.f;
+  for (int d = 0; d < DT; ++d)
 #pragma unroll
-    for (int d = 0; d < DT; ++d) o[q][d] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
+    for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
 
-  // ---- staging: pages of a tile's four times 16 tokens (scalar), codes and scales in registers, then bf16 in LDS
-  const int P1 = (1 << a.c.page_shift) - 1, last16 = (len - 1) & ~15;
+  // ---- staging: codes and scales of a tile in registers, then bf16 in LDS
+  const int shift = a.c.page_shift, P1 = (1 << shift) - 1, last16 = (len - 1) & ~15;
   const int32_t* table = a.c.table + (size_t)b * a.c.table_pages;
-  struct Pages { int p[4]; };
+  struct Pages { int p[4]; };                                // of a tile's four times 16 tokens; past the end the last ones
   auto pages_of = [&](int tile) {
-    Pages r;
+    Pages out;
+    if (shift >= 6) {
+      const int p = table[(tile * kAttnTile) >> shift];
+      out.p[0] = out.p[1] = out.p[2] = out.p[3] = (unsigned)p < (unsigned)a.c.n_pages ? p : -1;
+    } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int p = table[min(tile * kAttnTile + 16 * i, last16) >> a.c.page_shift];
-      r.p[i] = (unsigned)p < (unsigned)a.c.n_pages ? p : -1;
+      for (int i = 0; i < 4; ++i) {
+        const int p = table[min(tile * kAttnTile + 16 * i, last16) >> shift];
+        out.p[i] = (unsigned)p < (unsigned)a.c.n_pages ? p : -1;
+      }
     }
-    return r;
+    return out;
   };
   auto valid_of = [&](int tile, const Pages& pg) {
     const int left = len - tile * kAttnTile;
@@ -126,51 +125,150 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attention_rows_kernel(AttnA
       if (pg.p[i] < 0) v &= ~(0xFFFFull << (16 * i));
     return v;
   };
-  auto pick = [&](const Pages& pg, int i) { return i == 0 ? pg.p[0] : i == 1 ? pg.p[1] : i == 2 ? pg.p[2] : pg.p[3]; };
-  uint4 kc[T::PIECES], vc[T::PIECES];
-  float sc = 0.f;
+  auto pick = [&](const Pages& pg, int i) { return max(i == 0 ? pg.p[0] : i == 1 ? pg.p[1] : i == 2 ? pg.p[2] : pg.p[3], 0); };
+  uint4 kc[PIECES], vc[PIECES];
+  float sc[SC];
   constexpr int KP = DH / 16;                                // pieces of a key row
   auto load = [&](int tile, const Pages& pg) {
     const int j0 = tile * kAttnTile;
+    if (shift >= 6) {                                        // one page: its start is the same for all threads
+      const size_t page0 = codes_at<DH>(a.c, max(pg.p[0], 0), g), scale0 = scales_at<DH>(a.c, max(pg.p[0], 0), g);
+      const int place = j0 & P1;                             // the rest of the page is there, whether written or not
+      const int8_t* k0 = a.c.k_codes + page0 + (size_t)place * DH;
+      const int8_t* v0 = a.c.v_codes + page0 + place;
 #pragma unroll
-    for (int i = 0; i < T::PIECES; ++i) {
-      const int idx = threadIdx.x + i * kThreads, key = idx / KP, piece = idx % KP;
-      const int place = min(j0 + key, last16 + 15) & P1;
-      kc[i] = *reinterpret_cast<const uint4*>(a.c.k_codes + codes_at<DH>(a.c, max(pick(pg, key >> 4), 0), g) + (size_t)place * DH + piece * 16);
+      for (int i = 0; i < PIECES; ++i) kc[i] = *reinterpret_cast<const uint4*>(k0 + (threadIdx.x + i * THREADS) * 16);
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) {
+        const uint32_t idx = threadIdx.x + i * THREADS;
+        vc[i] = *reinterpret_cast<const uint4*>(v0 + (((idx >> 2) << shift) + (idx & 3) * 16));
+      }
+#pragma unroll
+      for (int i = 0; i < SC; ++i) {
+        const uint32_t idx = threadIdx.x + i * THREADS, blk = (idx >> 6) % NB;
+        if (SCALES % THREADS == 0 || idx < SCALES)
+          sc[i] = block_scale_load(idx < NB * 64 ? a.c.k_scales : a.c.v_scales, scale0 + (blk << shift) + place + (idx & 63), S16);
+      }
+      return;
     }
 #pragma unroll
-    for (int i = 0; i < T::PIECES; ++i) {
-      const int idx = threadIdx.x + i * kThreads, d = idx >> 2, piece = idx & 3;
-      const int place = min(j0 + piece * 16, last16) & P1;
-      vc[i] = *reinterpret_cast<const uint4*>(a.c.v_codes + codes_at<DH>(a.c, max(pick(pg, piece), 0), g) + ((size_t)d << a.c.page_shift) + place);
+    for (int i = 0; i < PIECES; ++i) {
+      const int idx = threadIdx.x + i * THREADS, key = idx / KP, piece = idx % KP, place = min(j0 + key, last16 + 15) & P1;
+      kc[i] = *reinterpret_cast<const uint4*>(a.c.k_codes + codes_at<DH>(a.c, pick(pg, key >> 4), g) + place * DH + piece * 16);
     }
-    if (threadIdx.x < 2 * NB * 64) {
-      const int key = threadIdx.x & 63, blk = (threadIdx.x >> 6) % NB;
-      const int page = pick(pg, key >> 4), place = min(j0 + key, last16 + 15) & P1;
-      const size_t at = scales_at<DH>(a.c, max(page, 0), g) + ((size_t)blk << a.c.page_shift) + place;
-      sc = block_scale_load(threadIdx.x < NB * 64 ? a.c.k_scales : a.c.v_scales, at, S16);
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      const int idx = threadIdx.x + i * THREADS, d = idx >> 2, piece = idx & 3, place = min(j0 + piece * 16, last16) & P1;
+      vc[i] = *reinterpret_cast<const uint4*>(a.c.v_codes + codes_at<DH>(a.c, pick(pg, piece), g) + (d << shift) + place);
+    }
+#pragma unroll
+    for (int i = 0; i < SC; ++i) {
+      const int idx = threadIdx.x + i * THREADS, key = idx & 63, blk = (idx >> 6) % NB, place = min(j0 + key, last16 + 15) & P1;
+      if (SCALES % THREADS == 0 || idx < SCALES)
+        sc[i] = block_scale_load(idx < NB * 64 ? a.c.k_scales : a.c.v_scales,
+                                 scales_at<DH>(a.c, pick(pg, key >> 4), g) + (blk << shift) + place, S16);
     }
   };
   const float factor = (DH == 64 ? 0.125f : 0.08838834764831845f) * kLog2e;
-  auto store = [&](typename T::Stage& st) {
+  auto store = [&](St& st) {
 #pragma unroll
-    for (int i = 0; i < T::PIECES; ++i) {
-      const int idx = threadIdx.x + i * kThreads, key = idx / KP, piece = idx % KP;
+    for (int i = 0; i < PIECES; ++i) {
+      const int idx = threadIdx.x + i * THREADS, key = idx / KP, piece = idx % KP;
       const uint2 w0 = codes4(kc[i].x), w1 = codes4(kc[i].y), w2 = codes4(kc[i].z), w3 = codes4(kc[i].w);
-      st.k[T::k_at(key, 2 * piece)] = make_uint4(w0.x, w0.y, w1.x, w1.y);
-      st.k[T::k_at(key, 2 * piece + 1)] = make_uint4(w2.x, w2.y, w3.x, w3.y);
+      st.k[St::k_at(key, 2 * piece)] = make_uint4(w0.x, w0.y, w1.x, w1.y);
+      st.k[St::k_at(key, 2 * piece + 1)] = make_uint4(w2.x, w2.y, w3.x, w3.y);
     }
 #pragma unroll
-    for (int i = 0; i < T::PIECES; ++i) {
-      const int idx = threadIdx.x + i * kThreads, d = idx >> 2, piece = idx & 3;
+    for (int i = 0; i < PIECES; ++i) {
+      const int idx = threadIdx.x + i * THREADS, d = idx >> 2, piece = idx & 3;
       const uint2 w0 = codes4(vc[i].x), w1 = codes4(vc[i].y), w2 = codes4(vc[i].z), w3 = codes4(vc[i].w);
-      st.v[T::v_at(d, 2 * piece)] = make_uint4(w0.x, w0.y, w1.x, w1.y);
-      st.v[T::v_at(d, 2 * piece + 1)] = make_uint4(w2.x, w2.y, w3.x, w3.y);
+      st.v[St::v_at(d, 2 * piece)] = make_uint4(w0.x, w0.y, w1.x, w1.y);
+      st.v[St::v_at(d, 2 * piece + 1)] = make_uint4(w2.x, w2.y, w3.x, w3.y);
     }
-    if (threadIdx.x < 2 * NB * 64) {
-      const int key = threadIdx.x & 63, blk = (threadIdx.x >> 6) % NB;
-      if (threadIdx.x < NB * 64) st.ks[blk][key] = sc * factor;
-      else st.vs[blk][key] = sc;
+#pragma unroll
+    for (int i = 0; i < SC; ++i) {
+      const int idx = threadIdx.x + i * THREADS, key = idx & 63, blk = (idx >> 6) % NB;
+      if (idx < NB * 64) st.ks[blk][key] = sc[i] * factor;
+      else if (SCALES % THREADS == 0 || idx < SCALES) st.vs[blk][key] = sc[i];
+    }
+  };
+
+  // 32 tokens of a tile: scores, weights, output
+  const int k_row = (n & 16) | ((n & 4) << 1) | ((n & 8) >> 1) | (n & 3);       // the token of this lane's row of the keys' operand
+  auto half = [&](const St& st, int j0, int kh, uint64_t valid) {
+    f32x16 acc[NB];
+#pragma unroll
+    for (int blk = 0; blk < NB; ++blk)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[blk][e] = 0.f;
+#pragma unroll
+    for (int k = 0; k < KK; ++k) {
+      const bf16x8 kf = __builtin_bit_cast(bf16x8, st.k[St::k_at(32 * kh + k_row, 2 * k + lh)]);
+      acc[k / 4] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[k], acc[k / 4], 0, 0, 0);
+    }
+    float p[16];                                             // tokens 32 kh + 16 (e / 8) + 8 lh + e % 8
+#pragma unroll
+    for (int e = 0; e < 16; e += 4) {
+      const int at = 32 * kh + 16 * (e >> 3) + 8 * lh + (e & 4);
+      const float4 k0 = *reinterpret_cast<const float4*>(&st.ks[0][at]);
+      p[e] = acc[0][e] * k0.x; p[e + 1] = acc[0][e + 1] * k0.y; p[e + 2] = acc[0][e + 2] * k0.z; p[e + 3] = acc[0][e + 3] * k0.w;
+      if constexpr (NB == 2) {
+        const float4 k1 = *reinterpret_cast<const float4*>(&st.ks[NB - 1][at]);
+        p[e] = fmaf(acc[NB - 1][e], k1.x, p[e]); p[e + 1] = fmaf(acc[NB - 1][e + 1], k1.y, p[e + 1]);
+        p[e + 2] = fmaf(acc[NB - 1][e + 2], k1.z, p[e + 2]); p[e + 3] = fmaf(acc[NB - 1][e + 3], k1.w, p[e + 3]);
+      }
+    }
+    const int h0 = j0 + 32 * kh;
+    const bool whole = (uint32_t)(valid >> (32 * kh)) == 0xFFFFFFFFu && h0 + 32 <= inner;
+    uint32_t sees = 0xFFFFFFFFu;                             // of the lane's query, by token
+    if (!whole) {
+      const int below = limit - h0;
+      sees = below >= 32 ? 0xFFFFFFFFu : below <= 0 ? 0u : (1u << below) - 1;
+      const int u0 = h0 - s.past;                            // of the first of them among the new tokens
+      if (u0 > -32 && u0 < 64) sees |= u0 >= 0 ? (uint32_t)(among >> u0) : (uint32_t)(among << -u0);
+      sees = (sees & (uint32_t)(valid >> (32 * kh))) >> (8 * lh);
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (!((sees >> (16 * (e >> 3) + (e & 7))) & 1)) p[e] = -INFINITY;
+    }
+    float top = fmaxf(p[0], p[1]);
+#pragma unroll
+    for (int e = 2; e < 16; ++e) top = fmaxf(top, p[e]);
+    if (__ballot(top > m + 8.0f)) {
+      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      const float mn = fmaxf(m, top);
+      const float keep = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      l *= keep;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o[d] *= keep;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      p[e] = __builtin_amdgcn_exp2f(p[e] - ref);
+      l += p[e];
+    }
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      bf16x8 pf[NB];
+#pragma unroll
+      for (int blk = 0; blk < NB; ++blk) {
+        const float4 s0 = *reinterpret_cast<const float4*>(&st.vs[blk][32 * kh + 16 * c + 8 * lh]);
+        const float4 s1 = *reinterpret_cast<const float4*>(&st.vs[blk][32 * kh + 16 * c + 8 * lh + 4]);
+        float w[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          w[e] *= p[8 * c + e];
+          if (!whole && !((sees >> (16 * c + e)) & 1)) w[e] = 0.f;     // the scale of a token that is not seen may be no number
+        }
+        pf[blk] = __builtin_bit_cast(bf16x8, make_uint4(pack2(w[0], w[1]), pack2(w[2], w[3]), pack2(w[4], w[5]), pack2(w[6], w[7])));
+      }
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        const bf16x8 vf = __builtin_bit_cast(bf16x8, st.v[St::v_at(d * 32 + n, 4 * kh + 2 * c + lh)]);
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[d / 2], o[d], 0, 0, 0);
+      }
     }
   };
 
@@ -190,106 +288,12 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attention_rows_kernel(AttnA
         if (tile + 2 < end) pg = pages_of(tile + 2);
       }
       const int j0 = tile * kAttnTile;
-      if (j0 < outer) {
-        const typename T::Stage& st = stage[(tile - first) & 1];
-        // ---- scores
-        float p[NQ][16];
-#pragma unroll
-        for (int hu = 0; hu < 4; ++hu) {
-          const int h = hu >> 1, u = hu & 1, key = 32 * h + 8 * (n >> 2) + 4 * u + (n & 3);
-          f32x4 acc[NQ][NB];
-#pragma unroll
-          for (int q = 0; q < NQ; ++q)
-#pragma unroll
-            for (int blk = 0; blk < NB; ++blk) acc[q][blk] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int k = 0; k < KK; ++k) {
-            const bf16x8 kf = __builtin_bit_cast(bf16x8, st.k[T::k_at(key, k * 4 + lg)]);
-#pragma unroll
-            for (int q = 0; q < NQ; ++q) acc[q][k / 2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[q][k], acc[q][k / 2], 0, 0, 0);
-          }
-          float4 ks[NB];
-#pragma unroll
-          for (int blk = 0; blk < NB; ++blk) ks[blk] = *reinterpret_cast<const float4*>(&st.ks[blk][32 * h + 8 * lg + 4 * u]);
-#pragma unroll
-          for (int q = 0; q < NQ; ++q) {
-            float* to = p[q] + h * 8 + u * 4;
-            to[0] = acc[q][0][0] * ks[0].x; to[1] = acc[q][0][1] * ks[0].y; to[2] = acc[q][0][2] * ks[0].z; to[3] = acc[q][0][3] * ks[0].w;
-            if constexpr (NB == 2) {
-              to[0] = fmaf(acc[q][1][0], ks[1].x, to[0]); to[1] = fmaf(acc[q][1][1], ks[1].y, to[1]);
-              to[2] = fmaf(acc[q][1][2], ks[1].z, to[2]); to[3] = fmaf(acc[q][1][3], ks[1].w, to[3]);
-            }
-          }
-        }
-        const bool whole = valid == ~0ull && j0 + kAttnTile <= inner;
-        uint64_t sees[NQ];
-#pragma unroll
-        for (int q = 0; q < NQ; ++q) sees[q] = ~0ull;
-        if (!whole) {
-#pragma unroll
-          for (int q = 0; q < NQ; ++q) {
-            const int below = limit[q] - j0;
-            uint64_t v = below >= 64 ? ~0ull : below <= 0 ? 0ull : (1ull << below) - 1;
-            const int shift = j0 - s.past;                       // of the first new token's bit
-            if (shift > -64 && shift < 64) v |= shift >= 0 ? among[q] >> shift : among[q] << -shift;
-            sees[q] = v & valid;
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-              if (!((sees[q] >> (32 * (e >> 3) + 8 * lg + (e & 7))) & 1)) p[q][e] = -INFINITY;
-          }
-        }
-        // ---- softmax
-#pragma unroll
-        for (int q = 0; q < NQ; ++q) {
-          float top = p[q][0];
-#pragma unroll
-          for (int e = 1; e < 16; ++e) top = fmaxf(top, p[q][e]);
-          if (__ballot(top > m[q] + 8.0f)) {
-            top = fmaxf(top, __shfl_xor(top, 16, 64));
-            top = fmaxf(top, __shfl_xor(top, 32, 64));
-            const float mn = fmaxf(m[q], top);
-            const float keep = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[q] - mn);
-            m[q] = mn;
-            l[q] *= keep;
-#pragma unroll
-            for (int d = 0; d < DT; ++d) o[q][d] *= keep;
-          }
-          const float ref = m[q] == -INFINITY ? 0.f : m[q];
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            p[q][e] = __builtin_amdgcn_exp2f(p[q][e] - ref);
-            l[q] += p[q][e];
-          }
-        }
-        // ---- output
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          bf16x8 pf[NQ][NB];
-#pragma unroll
-          for (int blk = 0; blk < NB; ++blk) {
-            const float4 s0 = *reinterpret_cast<const float4*>(&st.vs[blk][32 * h + 8 * lg]);
-            const float4 s1 = *reinterpret_cast<const float4*>(&st.vs[blk][32 * h + 8 * lg + 4]);
-            const float vs[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
-#pragma unroll
-            for (int q = 0; q < NQ; ++q) {
-              float w[8];
-#pragma unroll
-              for (int e = 0; e < 8; ++e) w[e] = p[q][h * 8 + e] * vs[e];
-              if (!whole) {                                      // a scale that is no number, of a token that is not seen
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                  if (!((sees[q] >> (32 * h + 8 * lg + e)) & 1)) w[e] = 0.f;
-              }
-              pf[q][blk] = __builtin_bit_cast(bf16x8, make_uint4(pack2(w[0], w[1]), pack2(w[2], w[3]), pack2(w[4], w[5]), pack2(w[6], w[7])));
-            }
-          }
-#pragma unroll
-          for (int d = 0; d < DT; ++d) {
-            const bf16x8 vf = __builtin_bit_cast(bf16x8, st.v[T::v_at(d * 16 + n, h * 4 + lg)]);
-#pragma unroll
-            for (int q = 0; q < NQ; ++q) o[q][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[q][d / 4], o[q][d], 0, 0, 0);
-          }
-        }
+      const St& st = stage[(tile - first) & 1];
+      if constexpr (KW == 1) {
+        if (j0 < outer) half(st, j0, 0, valid);
+        if (j0 + 32 < outer) half(st, j0, 1, valid);
+      } else {
+        if (j0 + 32 * key_wave < outer) half(st, j0, key_wave, valid);
       }
       if (more) store(stage[(tile + 1 - first) & 1]);
       valid = valid_next;
@@ -297,53 +301,71 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attention_rows_kernel(AttnA
     }
   }
 
+  l += __shfl_xor(l, 32, 64);
+  if constexpr (KW == 2) {                                   // the second half's results through LDS: [row wavefront][register][lane]
+    float* other = reinterpret_cast<float*>(lds) + row_wave * (DT * 16 + 2) * 64 + lane;
+    if (key_wave == 1) {
 #pragma unroll
-  for (int q = 0; q < NQ; ++q) {
-    float total = l[q];
-    total += __shfl_xor(total, 16, 64);
-    total += __shfl_xor(total, 32, 64);
-    const int r = w0 + q * 16 + n;
-    if (r >= rows) continue;
-    if (a.splits == 1) {
-      const int t = r / a.group, h = r - t * a.group;
-      bf16_raw* to = reinterpret_cast<bf16_raw*>(a.out) + ((size_t)b * a.c.tokens + t) * a.out_pitch + (size_t)(g * a.group + h) * DH + 4 * lg;
-      const float f = total == 0.f ? 0.f : 1.0f / total;
+      for (int d = 0; d < DT; ++d)
 #pragma unroll
-      for (int d = 0; d < DT; ++d) {
-        const f32x4 y = o[q][d];
-        *reinterpret_cast<uint2*>(to + d * 16) =
-            total == 0.f ? make_uint2(0, 0) : make_uint2(pack2(y[0] * f, y[1] * f), pack2(y[2] * f, y[3] * f));
-      }
-    } else {
-      const size_t at = ((((size_t)b * a.row_groups + rg) * a.c.KV + g) * a.splits + split) * Q + (r - r0);
-#pragma unroll
-      for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(a.part_o + at * DH + d * 16 + 4 * lg) = o[q][d];
-      if (lg == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = make_float2(m[q], total);
+        for (int e = 0; e < 16; ++e) other[(d * 16 + e) * 64] = o[d][e];
+      other[DT * 16 * 64] = m;
+      other[(DT * 16 + 1) * 64] = l;
     }
+    __syncthreads();
+    if (key_wave == 1) return;
+    const float m1 = other[DT * 16 * 64], mn = fmaxf(m, m1), ref = mn == -INFINITY ? 0.f : mn;
+    const float f0 = __builtin_amdgcn_exp2f(m - ref), f1 = __builtin_amdgcn_exp2f(m1 - ref);
+    m = mn;
+    l = fmaf(other[(DT * 16 + 1) * 64], f1, l * f0);
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[d][e] = fmaf(other[(d * 16 + e) * 64], f1, o[d][e] * f0);
+  }
+  if (!real) return;
+  if (a.splits == 1) {
+    bf16_raw* to = reinterpret_cast<bf16_raw*>(a.out) + row * a.out_pitch + (size_t)head * DH + 4 * lh;
+    const float f = l == 0.f ? 0.f : 1.0f / l;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4)
+        *reinterpret_cast<uint2*>(to + d * 32 + 2 * e) =
+            l == 0.f ? make_uint2(0, 0) : make_uint2(pack2(o[d][e] * f, o[d][e + 1] * f), pack2(o[d][e + 2] * f, o[d][e + 3] * f));
+  } else {
+    const size_t at = ((((size_t)b * a.row_groups + rg) * a.c.KV + g) * a.splits + split) * Q + (r - r0);
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4)
+        *reinterpret_cast<float4*>(a.part_o + at * DH + d * 32 + 2 * e + 4 * lh) = make_float4(o[d][e], o[d][e + 1], o[d][e + 2], o[d][e + 3]);
+    if (lh == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = make_float2(m, l);
   }
 }
 
-template <int DH, int NQ, bool S16>
+template <int DH, int RW, int KW, bool S16>
 swarm_status launch(const AttnArgs& a, hipStream_t st) {
   static LdsOptIn opted;
-  constexpr size_t bytes = 2 * sizeof(typename Tiles<DH>::Stage);
-  const swarm_status ok = lds_opt_in(reinterpret_cast<const void*>(&cache_attention_rows_kernel<DH, NQ, S16>), bytes, opted);
+  constexpr size_t bytes = 2 * sizeof(Stage<DH>);
+  static_assert(KW == 1 || RW * (DH / 2 + 2) * 64 * 4 <= (int)bytes, "the second half's results fit where the tiles were");
+  const swarm_status ok = lds_opt_in(reinterpret_cast<const void*>(&cache_attention_rows_kernel<DH, RW, KW, S16>), bytes, opted);
   if (ok != SWARM_OK) return ok;
   const long long pairs = ((long long)a.c.B * a.c.KV + 7) / 8 * 8, blocks = pairs * a.row_groups * a.splits;
   if (blocks > 0x7FFFFFFF) return SWARM_ERR_SHAPE;
-  hipLaunchKernelGGL((cache_attention_rows_kernel<DH, NQ, S16>), dim3((unsigned)blocks), dim3(kThreads), bytes, st, a);
+  hipLaunchKernelGGL((cache_attention_rows_kernel<DH, RW, KW, S16>), dim3((unsigned)blocks), dim3(64 * RW * KW), bytes, st, a);
   return launch_status();
+}
+template <int DH, bool S16>
+swarm_status launch_rows(const AttnArgs& a, int row_waves, hipStream_t st) {
+  return row_waves == 2 ? launch<DH, 2, 2, S16>(a, st) : launch<DH, 4, 1, S16>(a, st);
 }
 
 }  // namespace
 
-swarm_status cache_attention_rows_launch(const AttnArgs& a, int dh, int tiles, hipStream_t st) {
-  if (dh == 64) {
-    if (tiles == 1) return a.s16 ? launch<64, 1, true>(a, st) : launch<64, 1, false>(a, st);
-    return a.s16 ? launch<64, 2, true>(a, st) : launch<64, 2, false>(a, st);
-  }
-  if (tiles == 1) return a.s16 ? launch<128, 1, true>(a, st) : launch<128, 1, false>(a, st);
-  return a.s16 ? launch<128, 2, true>(a, st) : launch<128, 2, false>(a, st);
+swarm_status cache_attention_rows_launch(const AttnArgs& a, int dh, int row_waves, hipStream_t st) {
+  if (dh == 64) return a.s16 ? launch_rows<64, true>(a, row_waves, st) : launch_rows<64, false>(a, row_waves, st);
+  return a.s16 ? launch_rows<128, true>(a, row_waves, st) : launch_rows<128, false>(a, row_waves, st);
 }
 
 }  // namespace swarm
