@@ -110,10 +110,9 @@ class CacheConfig:
             dtype = {torch.float32: SWARM_F32, torch.bfloat16: SWARM_BF16}[dtype]
         self.c = _CacheConfig(n_heads, n_kv_heads, d_head, page_tokens, n_pages, batch, table_pages, dtype, scale_bits)
         self._ref = C.byref(self.c)
-
-    @property
-    def torch_dtype(self):
-        return torch.float32 if self.c.dtype == SWARM_F32 else torch.bfloat16
+        self.torch_dtype = torch.float32 if dtype == SWARM_F32 else torch.bfloat16
+        self._pool = (n_kv_heads, d_head, page_tokens, n_pages, scale_bits)        # what a Cache of it has to be made for
+        self._sizes = (batch, batch * table_pages, n_heads * d_head, n_kv_heads * d_head, self.torch_dtype)
 
     def shapes(self):
         """Shape and dtype of the four tensors of a Cache (16-bit scales are bf16 values)."""
@@ -136,8 +135,14 @@ class Cache:
                 raise ValueError("%s has shape %s, the cache has %s" % (name, tuple(t.shape), shape))
             if t.dtype != dtype and not (t.element_size() == 2 and dtype == torch.bfloat16):
                 raise TypeError("%s must be %s" % (name, dtype))
-        self.layout = bytes(cfg.c)
-        self.c = _Cache(*(_on_device(t) for t in self.tensors.values()))
+            if not t.is_contiguous():
+                raise ValueError("%s must be contiguous" % name)
+        devices = {t.get_device() for t in self.tensors.values()}
+        if len(devices) != 1:
+            raise ValueError("the tensors of a cache must be on one device")
+        self._device = devices.pop()
+        self._pool = cfg._pool
+        self.c = _Cache(*(t.data_ptr() for t in self.tensors.values()))
         self._ref = C.byref(self.c)
 
 
@@ -170,8 +175,14 @@ class LogitsRules:
                 raise TypeError("%s must be fp32" % name)
             if tuple(t.shape) != (whole.get(name) or real.get(name)):
                 raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), whole.get(name) or real.get(name)))
+            if not t.is_contiguous():
+                raise ValueError("%s must be contiguous" % name)
+        devices = {t.get_device() for t in given.values() if t is not None}
+        if len(devices) > 1:
+            raise ValueError("the tensors of the rules must be on one device")
         self.tensors = given
-        self.c = _LogitsRules(rows, vocab, n_history, n_bias, *(_on_device(t) for t in given.values()))
+        self._sizes = (rows, vocab, devices.pop() if devices else None)
+        self.c = _LogitsRules(rows, vocab, n_history, n_bias, *(None if t is None else t.data_ptr() for t in given.values()))
         self._ref = C.byref(self.c)
 
 
@@ -344,43 +355,6 @@ def _ptr(t: Optional[torch.Tensor]):
     return t.data_ptr()
 
 
-def _on_device(t: Optional[torch.Tensor]):
-    """_ptr of a tensor that a kernel will read: it has to lie on the current GPU (any tensor where there is no GPU at all)."""
-    if t is None:
-        return None
-    if not t.is_contiguous():
-        raise ValueError("tensors passed to the stage library must be contiguous")
-    if _current_device is not None and torch.cuda.is_initialized() and t.get_device() != _current_device():
-        raise ValueError("a tensor is on %s, the current GPU is %d" % (t.device, _current_device()))
-    return t.data_ptr()
-
-
-def _rows(t: Optional[torch.Tensor], rows: int, width: int, dtype: torch.dtype, name: str):
-    """(pointer, pitch in elements) of a [rows, width] tensor whose rows may lie further apart."""
-    if t is None:
-        return None, 0
-    if t.dtype != dtype:
-        raise TypeError("%s must be %s" % (name, dtype))
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != width:
-        raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), (rows, width)))
-    if width > 1 and t.stride(1) != 1:
-        raise ValueError("the elements of a row of %s must be contiguous" % name)
-    if _current_device is not None and torch.cuda.is_initialized() and t.get_device() != _current_device():
-        raise ValueError("%s is on %s, the current GPU is %d" % (name, t.device, _current_device()))
-    return t.data_ptr(), (t.stride(0) if rows > 1 else max(width, t.stride(0)))
-
-
-def _ints(t: Optional[torch.Tensor], n: int, name: str):
-    """Pointer of a contiguous int32 tensor of n elements."""
-    if t is None:
-        return None
-    if t.dtype != torch.int32:
-        raise TypeError("%s must be int32" % name)
-    if t.numel() != n:
-        raise ValueError("%s has %d elements, expected %d" % (name, t.numel(), n))
-    return _on_device(t)
-
-
 # The current stream's handle without the torch.cuda.Stream object around it, which takes longer to make than a launch (a call
 # of a small kernel 7.5 -> 5.0 us); where torch has no such functions, or CUDA is not initialised yet, the object is made.
 _current_device = getattr(torch._C, "_cuda_getDevice", None)
@@ -395,6 +369,77 @@ def _stream(stream) -> Optional[int]:
     if isinstance(stream, int):
         return stream or None
     return stream.cuda_stream or None
+
+
+# The calls of token-by-token generation are as short as a launch, so their checks ask each tensor as little as they can: type, size,
+# contiguity and device in one condition, and what is wrong only once something is.
+_I32, _F32 = torch.int32, torch.float32
+_WORDS = tuple(getattr(torch, n) for n in ("int64", "uint64") if hasattr(torch, n))
+
+
+def _device() -> Optional[int]:
+    """The current GPU; None where there is none, or none has been used yet (so no tensor can lie on it)."""
+    return _current_device() if _current_device is not None and torch.cuda.is_initialized() else None
+
+
+def _refuse(t: torch.Tensor, name: str, dtypes, n: Optional[int], device: Optional[int]):
+    if t.dtype not in dtypes:
+        raise TypeError("%s must be %s" % (name, " or ".join(str(d) for d in dtypes)))
+    if n is not None and t.numel() != n:
+        raise ValueError("%s has %d elements, expected %d" % (name, t.numel(), n))
+    if not t.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+    raise ValueError("%s is on %s, not on the current GPU (%s)" % (name, t.device, device))
+
+
+def _ints(t: Optional[torch.Tensor], n: int, name: str, device: Optional[int]):
+    """Pointer of n int32 values."""
+    if t is None:
+        return None
+    if t.dtype is not _I32 or t.numel() != n or not t.is_contiguous() or t.get_device() != device:
+        _refuse(t, name, (_I32,), n, device)
+    return t.data_ptr()
+
+
+def _buffer(t: torch.Tensor, n: Optional[int], dtype: torch.dtype, name: str, device: Optional[int]):
+    """Pointer of n (None: any number of) values of a type."""
+    if t.dtype is not dtype or (n is not None and t.numel() != n) or not t.is_contiguous() or t.get_device() != device:
+        _refuse(t, name, (dtype,), n, device)
+    return t.data_ptr()
+
+
+def _rows(t: torch.Tensor, rows: int, width: int, dtype: torch.dtype, name: str, device: Optional[int]):
+    """(pointer, pitch in elements) of a [rows, width] tensor whose rows may lie further apart; a single row has the pitch `width`."""
+    if t.dtype is not dtype:
+        raise TypeError("%s must be %s" % (name, dtype))
+    if t.shape != (rows, width):
+        raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), (rows, width)))
+    pitch, step = t.stride()
+    if step != 1 and width > 1:
+        raise ValueError("the elements of a row of %s must be contiguous" % name)
+    if t.get_device() != device:
+        _refuse(t, name, (dtype,), None, device)
+    return t.data_ptr(), (pitch if rows > 1 else width)
+
+
+def _tree(tree: Optional[torch.Tensor], rows: int, device: Optional[int]):
+    if tree is None:
+        return None
+    if tree.dtype not in _WORDS or tree.numel() != rows or not tree.is_contiguous() or tree.get_device() != device:
+        _refuse(tree, "tree", _WORDS, rows, device)
+    return tree.data_ptr()
+
+
+def _workspace(t: Optional[torch.Tensor], device: Optional[int]):
+    """(pointer, bytes); an empty workspace is none."""
+    if t is None:
+        return None, 0
+    n = t.numel() * t.element_size()
+    if n == 0:
+        return None, 0
+    if not t.is_contiguous() or t.get_device() != device:
+        _refuse(t, "workspace", (t.dtype,), None, device)
+    return t.data_ptr(), n
 
 
 def _dtype_code(t: torch.Tensor) -> int:
@@ -659,23 +704,12 @@ def swarm_lamb_step_static(master: torch.Tensor, param: Optional[torch.Tensor], 
         raise SwarmError(st, "swarm_lamb_step_static")
 
 
-def _pool(cfg: CacheConfig, cache: Cache):
-    if cache.layout != bytes(cfg.c):
-        a = _CacheConfig.from_buffer_copy(cache.layout)
-        same = ("n_kv_heads", "d_head", "page_tokens", "n_pages", "scale_bits")
-        if any(getattr(a, k) != getattr(cfg.c, k) for k in same):
-            raise ValueError("the cache was made for another configuration")
+def _pool(cfg: CacheConfig, cache: Cache, device: Optional[int]):
+    if cache._pool != cfg._pool:
+        raise ValueError("the cache was made for another configuration")
+    if cache._device != device:
+        raise ValueError("the cache is on GPU %d, the current GPU is %s" % (cache._device, device))
     return cache._ref
-
-
-def _tree(tree: Optional[torch.Tensor], rows: int):
-    if tree is None:
-        return None
-    if tree.dtype not in (torch.int64, getattr(torch, "uint64", torch.int64)):
-        raise TypeError("tree must be a 64-bit tensor")
-    if tree.numel() != rows:
-        raise ValueError("tree has %d words, expected %d" % (tree.numel(), rows))
-    return _on_device(tree)
 
 
 def swarm_cache_append(cfg: CacheConfig, cache: Cache, page_table: torch.Tensor, past: torch.Tensor,
@@ -683,44 +717,45 @@ def swarm_cache_append(cfg: CacheConfig, cache: Cache, page_table: torch.Tensor,
                        q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
                        positions: Optional[torch.Tensor] = None, rotary: bool = False, stream=None) -> None:
     """q, k, v: [batch * tokens, heads * d_head] views of one row pitch (the columns of a fused product)."""
-    c = cfg.c
-    rows, dt = c.batch * tokens, cfg.torch_dtype
-    kp, pitch = _rows(k, rows, c.n_kv_heads * c.d_head, dt, "k")
-    vp, v_pitch = _rows(v, rows, c.n_kv_heads * c.d_head, dt, "v")
-    qp, q_pitch = _rows(q, rows, c.n_heads * c.d_head, dt, "q")
-    op, out_pitch = _rows(q_out, rows, c.n_heads * c.d_head, dt, "q_out")
-    if rows == 1:                       # a single row has no pitch
-        pitch = v_pitch = q_pitch = max(pitch, v_pitch, q_pitch)
-    if v_pitch != pitch or (q is not None and q_pitch != pitch):
+    batch, pages, q_width, kv_width, dt = cfg._sizes
+    rows, dev = batch * tokens, _device()
+    kp, pitch = _rows(k, rows, kv_width, dt, "k", dev)
+    vp, v_pitch = _rows(v, rows, kv_width, dt, "v", dev)
+    qp, q_pitch, op, out_pitch = None, pitch, None, 0
+    if q is not None:
+        qp, q_pitch = _rows(q, rows, q_width, dt, "q", dev)
+        if rows == 1:                   # a single row has no pitch
+            pitch = v_pitch = q_pitch
+    if q_out is not None:
+        op, out_pitch = _rows(q_out, rows, q_width, dt, "q_out", dev)
+    if v_pitch != pitch or q_pitch != pitch:
         raise ValueError("q, k and v must have the same row pitch")
-    st = load_library().swarm_cache_append(cfg._ref, _pool(cfg, cache), _ints(page_table, c.batch * c.table_pages, "page_table"),
-                                           _ints(past, c.batch, "past"), _ints(fresh, c.batch, "fresh"), tokens, qp, kp, vp, pitch,
-                                           _ints(positions, rows, "positions"), int(rotary), op, out_pitch, _stream(stream))
+    st = load_library().swarm_cache_append(cfg._ref, _pool(cfg, cache, dev), _ints(page_table, pages, "page_table", dev),
+                                           _ints(past, batch, "past", dev), _ints(fresh, batch, "fresh", dev), tokens, qp, kp, vp,
+                                           pitch, _ints(positions, rows, "positions", dev), 1 if rotary else 0, op, out_pitch,
+                                           _stream(stream))
     if st != 0:
         raise SwarmError(st, "swarm_cache_append")
 
 
 def swarm_cache_read(cfg: CacheConfig, cache: Cache, page_table: torch.Tensor, first: torch.Tensor,
                      count: Optional[torch.Tensor], tokens: int, k_out: torch.Tensor, v_out: torch.Tensor, stream=None) -> None:
-    c = cfg.c
-    for t in (k_out, v_out):
-        if t.dtype != cfg.torch_dtype:
-            raise TypeError("k_out and v_out must be %s" % cfg.torch_dtype)
-        if t.numel() != c.batch * tokens * c.n_kv_heads * c.d_head:
-            raise ValueError("k_out and v_out must have batch * tokens rows of n_kv_heads * d_head elements")
-    st = load_library().swarm_cache_read(cfg._ref, _pool(cfg, cache), _ints(page_table, c.batch * c.table_pages, "page_table"),
-                                         _ints(first, c.batch, "first"), _ints(count, c.batch, "count"), tokens,
-                                         _on_device(k_out), _on_device(v_out), _stream(stream))
+    batch, pages, _, kv_width, dt = cfg._sizes
+    n, dev = batch * tokens * kv_width, _device()
+    st = load_library().swarm_cache_read(cfg._ref, _pool(cfg, cache, dev), _ints(page_table, pages, "page_table", dev),
+                                         _ints(first, batch, "first", dev), _ints(count, batch, "count", dev), tokens,
+                                         _buffer(k_out, n, dt, "k_out", dev), _buffer(v_out, n, dt, "v_out", dev), _stream(stream))
     if st != 0:
         raise SwarmError(st, "swarm_cache_read")
 
 
 def swarm_cache_keep(cfg: CacheConfig, cache: Cache, page_table: torch.Tensor, past: torch.Tensor, kept: torch.Tensor,
                      n_kept: torch.Tensor, tokens: int, stream=None) -> None:
-    c = cfg.c
-    st = load_library().swarm_cache_keep(cfg._ref, _pool(cfg, cache), _ints(page_table, c.batch * c.table_pages, "page_table"),
-                                         _ints(past, c.batch, "past"), _ints(kept, c.batch * tokens, "kept"),
-                                         _ints(n_kept, c.batch, "n_kept"), tokens, _stream(stream))
+    batch, pages = cfg._sizes[:2]
+    dev = _device()
+    st = load_library().swarm_cache_keep(cfg._ref, _pool(cfg, cache, dev), _ints(page_table, pages, "page_table", dev),
+                                         _ints(past, batch, "past", dev), _ints(kept, batch * tokens, "kept", dev),
+                                         _ints(n_kept, batch, "n_kept", dev), tokens, _stream(stream))
     if st != 0:
         raise SwarmError(st, "swarm_cache_keep")
 
@@ -734,15 +769,14 @@ def swarm_cache_attention(cfg: CacheConfig, cache: Cache, page_table: torch.Tens
                           workspace: Optional[torch.Tensor], tree: Optional[torch.Tensor] = None, max_len: int = 0,
                           stream=None) -> None:
     """q, out: [batch * tokens, n_heads * d_head]; their rows may lie further apart."""
-    c = cfg.c
-    rows, width, dt = c.batch * tokens, c.n_heads * c.d_head, cfg.torch_dtype
-    qp, q_pitch = _rows(q, rows, width, dt, "q")
-    op, out_pitch = _rows(out, rows, width, dt, "out")
-    n = workspace.numel() * workspace.element_size() if workspace is not None else 0
-    st = load_library().swarm_cache_attention(cfg._ref, _pool(cfg, cache), _ints(page_table, c.batch * c.table_pages, "page_table"),
-                                              _ints(past, c.batch, "past"), _ints(fresh, c.batch, "fresh"), tokens, max_len, qp,
-                                              q_pitch, _tree(tree, rows), op, out_pitch, _on_device(workspace) if n else None, n,
-                                              _stream(stream))
+    batch, pages, width, _, dt = cfg._sizes
+    rows, dev = batch * tokens, _device()
+    qp, q_pitch = _rows(q, rows, width, dt, "q", dev)
+    op, out_pitch = _rows(out, rows, width, dt, "out", dev)
+    wp, n = _workspace(workspace, dev)
+    st = load_library().swarm_cache_attention(cfg._ref, _pool(cfg, cache, dev), _ints(page_table, pages, "page_table", dev),
+                                              _ints(past, batch, "past", dev), _ints(fresh, batch, "fresh", dev), tokens, max_len,
+                                              qp, q_pitch, _tree(tree, rows, dev), op, out_pitch, wp, n, _stream(stream))
     if st != 0:
         raise SwarmError(st, "swarm_cache_attention")
 
@@ -756,48 +790,45 @@ def swarm_stage_extend(cfg: StageConfig, params: List[Dict[str, torch.Tensor]], 
                        x_out: torch.Tensor, workspace: torch.Tensor, positions: Optional[torch.Tensor] = None,
                        tree: Optional[torch.Tensor] = None, max_len: int = 0, stream=None) -> None:
     """caches: one for each of the n_layers * n_repeat applications, in their order."""
-    c, cc = cfg.c, cache_cfg.c
+    c, dev = cfg.c, _device()
+    batch, pages = cache_cfg._sizes[:2]
     rows = c.batch * c.seq
     if len(params) != c.n_layers or len(caches) != c.n_layers * c.n_repeat:
         raise ValueError("the stage has %d parameter sets and %d applications" % (c.n_layers, c.n_layers * c.n_repeat))
-    for t in (x_in, x_out):
-        if t.dtype != cfg.torch_dtype or t.numel() != rows * c.d_model:
-            raise ValueError("x_in and x_out must be [batch * seq, d_model] of the stage's dtype")
     for pool in caches:
-        _pool(cache_cfg, pool)
+        _pool(cache_cfg, pool, dev)
     pools = (_Cache * len(caches))(*(pool.c for pool in caches))
+    wp, n = _workspace(workspace, dev)
     st = load_library().swarm_stage_extend(C.byref(c), _block_array(params), cache_cfg._ref, pools,
-                                           _ints(page_table, cc.batch * cc.table_pages, "page_table"),
-                                           _ints(past, cc.batch, "past"), _ints(fresh, cc.batch, "fresh"),
-                                           _ints(positions, rows, "positions"), _tree(tree, rows), max_len, _on_device(x_in),
-                                           _on_device(x_out), _on_device(workspace), workspace.numel() * workspace.element_size(),
-                                           _stream(stream))
+                                           _ints(page_table, pages, "page_table", dev), _ints(past, batch, "past", dev),
+                                           _ints(fresh, batch, "fresh", dev), _ints(positions, rows, "positions", dev),
+                                           _tree(tree, rows, dev), max_len, _buffer(x_in, rows * c.d_model, cfg.torch_dtype, "x_in", dev),
+                                           _buffer(x_out, rows * c.d_model, cfg.torch_dtype, "x_out", dev), wp, n, _stream(stream))
     if st != 0:
         raise SwarmError(st, "swarm_stage_extend")
 
 
 def swarm_head_logits(cfg: HeadConfig, params: Dict[str, torch.Tensor], x: torch.Tensor, logits: torch.Tensor,
                       workspace: torch.Tensor, stream=None) -> None:
-    if logits.dtype != x.dtype or _dtype_code(x) != cfg.c.dtype:
-        raise TypeError("x and logits must have the head's dtype")
-    if x.numel() != cfg.c.tokens * cfg.c.d_model or logits.numel() != cfg.c.tokens * cfg.c.vocab_rows:
-        raise ValueError("x must be [tokens, d_model] and logits [tokens, vocab_rows]")
-    st = load_library().swarm_head_logits(C.byref(cfg.c), C.byref(_ptrs3(params, "w_vocab")), _on_device(x), _on_device(logits),
-                                          _on_device(workspace), workspace.numel() * workspace.element_size(), _stream(stream))
+    c, dev = cfg.c, _device()
+    dt = torch.float32 if c.dtype == SWARM_F32 else torch.bfloat16
+    wp, n = _workspace(workspace, dev)
+    st = load_library().swarm_head_logits(C.byref(c), C.byref(_ptrs3(params, "w_vocab")), _buffer(x, c.tokens * c.d_model, dt, "x", dev),
+                                          _buffer(logits, c.tokens * c.vocab_rows, dt, "logits", dev), wp, n, _stream(stream))
     if st != 0:
         raise SwarmError(st, "swarm_head_logits")
 
 
 def swarm_logits_adjust(rules: LogitsRules, logits: torch.Tensor, out: torch.Tensor, stream=None) -> None:
     """logits [rows, >= vocab] fp32 or bf16, out [rows, >= vocab] fp32; rows may lie further apart."""
-    rows, vocab = rules.c.rows, rules.c.vocab
-    if out.dtype != torch.float32:
-        raise TypeError("out must be fp32")
-    for name, t in (("logits", logits), ("out", out)):
-        if t.dim() != 2 or t.shape[0] != rows or t.shape[1] < vocab:
-            raise ValueError("%s must be [rows, vocab or more]" % name)
-    lp, pitch = _rows(logits, rows, logits.shape[1], logits.dtype, "logits")
-    op, out_pitch = _rows(out, rows, out.shape[1], out.dtype, "out")
+    rows, vocab, rules_dev = rules._sizes
+    dev = _device()
+    if logits.dim() != 2 or logits.shape[1] < vocab or out.dim() != 2 or out.shape[1] < vocab:
+        raise ValueError("logits and out must be [rows, vocab or more]")
+    lp, pitch = _rows(logits, rows, logits.shape[1], logits.dtype, "logits", dev)
+    op, out_pitch = _rows(out, rows, out.shape[1], _F32, "out", dev)
+    if rules_dev is not None and rules_dev != dev:
+        raise ValueError("the rules are on GPU %d, the current GPU is %s" % (rules_dev, dev))
     st = load_library().swarm_logits_adjust(rules._ref, lp, _dtype_code(logits), pitch, op, out_pitch, _stream(stream))
     if st != 0:
         raise SwarmError(st, "swarm_logits_adjust")

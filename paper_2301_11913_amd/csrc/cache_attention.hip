@@ -339,47 +339,58 @@ __global__ __launch_bounds__(kThreads) void cache_attention_bytes_kernel(AttnArg
   }
 }
 
-// The splits of one row and head joined, one workgroup each: every d_head / 4 threads take the partial results of some of the splits,
-// eight (16 at d_head 64) at a time, and are added up in order.
+// The splits of a row and head joined.  d_head / 4 threads hold a row's elements; `slices` of them (a power of two, no more than
+// there are splits) share a row, each takes every slices-th split, and the slices are added up in order.  Many splits: one row per
+// workgroup; two: as many as fit.
 template <typename T, int DH>
-__global__ __launch_bounds__(kThreads) void cache_attention_join_kernel(AttnArgs a, int Q) {
+__global__ __launch_bounds__(kThreads) void cache_attention_join_kernel(AttnArgs a, int Q, int slices) {
   constexpr int LANES = DH / 4, SLICES = kThreads / LANES;
   __shared__ float4 sums[SLICES][LANES];
-  __shared__ float totals[SLICES], tops[kWaves];
-  const int h = blockIdx.x % a.c.H, row = blockIdx.x / a.c.H;
-  const int b = row / a.c.tokens, t = row - b * a.c.tokens, g = h / a.group;
-  if (t >= span_of(a.c, b).fresh) return;
+  __shared__ float tops[SLICES], totals[SLICES];
+  const int lane = threadIdx.x % LANES, slot = threadIdx.x / LANES, slice = slot & (slices - 1), per = SLICES / slices;
+  const long long unit = (long long)blockIdx.x * per + slot / slices;          // (row, head)
+  const int h = (int)(unit % a.c.H);
+  const long long row = unit / a.c.H;
+  const int b = (int)(row / a.c.tokens), t = (int)(row - (long long)b * a.c.tokens), g = h / a.group;
+  const bool real = b < a.c.B && t < span_of(a.c, min(b, a.c.B - 1)).fresh;
   const int r = t * a.group + h - g * a.group, rg = r / Q;
   const size_t at = (((size_t)b * a.row_groups + rg) * a.c.KV + g) * a.splits * Q + (r - rg * Q);
   float top = -INFINITY;
-  for (int p = threadIdx.x; p < a.splits; p += kThreads) top = fmaxf(top, a.part_ml[2 * (at + (size_t)p * Q)]);
-  top = wave_max(top);
-  if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+  if (real)
+    for (int p = slice + lane * slices; p < a.splits; p += LANES * slices) top = fmaxf(top, a.part_ml[2 * (at + (size_t)p * Q)]);
+#pragma unroll
+  for (int d = LANES / 2; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+  if (lane == 0) tops[slot] = top;
   __syncthreads();
-  top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+  for (int i = 0; i < slices; ++i) top = fmaxf(top, tops[slot - slice + i]);
   const float ref = top == -INFINITY ? 0.f : top;
-  const int lane = threadIdx.x % LANES, slice = threadIdx.x / LANES;
   float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
   float total = 0.f;
+  if (real) {
 #pragma unroll 4
-  for (int p = slice; p < a.splits; p += SLICES) {
-    const size_t k = at + (size_t)p * Q;
-    const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * k);
-    const float4 o = *reinterpret_cast<const float4*>(a.part_o + k * DH + lane * 4);
-    const float f = __builtin_amdgcn_exp2f(ml.x - ref);
-    total = fmaf(ml.y, f, total);
-    x.x = fmaf(o.x, f, x.x); x.y = fmaf(o.y, f, x.y); x.z = fmaf(o.z, f, x.z); x.w = fmaf(o.w, f, x.w);
+    for (int p = slice; p < a.splits; p += slices) {
+      const size_t k = at + (size_t)p * Q;
+      const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * k);
+      const float4 o = *reinterpret_cast<const float4*>(a.part_o + k * DH + lane * 4);
+      const float f = __builtin_amdgcn_exp2f(ml.x - ref);
+      total = fmaf(ml.y, f, total);
+      x.x = fmaf(o.x, f, x.x); x.y = fmaf(o.y, f, x.y); x.z = fmaf(o.z, f, x.z); x.w = fmaf(o.w, f, x.w);
+    }
   }
-  sums[slice][lane] = x;
-  if (lane == 0) totals[slice] = total;
+  sums[slot][lane] = x;
+  if (lane == 0) totals[slot] = total;
   __syncthreads();
-  if (threadIdx.x >= DH) return;
-  const int d = threadIdx.x;
-  float sum = 0.f;
-  total = 0.f;
+  if (slice || !real) return;
+  for (int i = 1; i < slices; ++i) {
+    const float4 y = sums[slot + i][lane];
+    x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+    total += totals[slot + i];
+  }
+  T* to = reinterpret_cast<T*>(a.out) + (size_t)row * a.out_pitch + (size_t)h * DH + lane * 4;
+  const float f = total == 0.f ? 0.f : 1.0f / total;
+  const float y[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-  for (int i = 0; i < SLICES; ++i) { sum += reinterpret_cast<const float*>(sums[i])[d]; total += totals[i]; }
-  Elem<T>::store(reinterpret_cast<T*>(a.out) + (size_t)row * a.out_pitch + (size_t)h * DH + d, total == 0.f ? 0.f : sum / total);
+  for (int i = 0; i < 4; ++i) Elem<T>::store(to + i, total == 0.f ? 0.f : y[i] * f);
 }
 
 // How the rows and the tokens of a call are cut.
@@ -442,8 +453,12 @@ swarm_status launch(const AttnArgs& a, const Cut& k, hipStream_t st) {
   } else {
     launch_bytes<T, DH, 4>(a, (unsigned)blocks, st);
   }
-  if (k.splits > 1)
-    hipLaunchKernelGGL((cache_attention_join_kernel<T, DH>), dim3((unsigned)joins), dim3(kThreads), 0, st, a, k.rows);
+  if (k.splits > 1) {
+    int slices = 1024 / DH;
+    while (slices > 1 && slices > k.splits) slices >>= 1;
+    const int per = 1024 / DH / slices;
+    hipLaunchKernelGGL((cache_attention_join_kernel<T, DH>), dim3((unsigned)((joins + per - 1) / per)), dim3(kThreads), 0, st, a, k.rows, slices);
+  }
   return launch_status();
 }
 }  // namespace

@@ -41,6 +41,7 @@ template <int DH> struct Stage {
   uint4 k[64 * CH];
   uint4 v[DH * 8];
   float ks[NB][64], vs[NB][64];                            // keys' with the factor of the scores in them
+  uint32_t bad[NB][2];                                     // tokens whose value's scale is no finite number; 0 stands in its place
   static __device__ __forceinline__ int k_at(int key, int chunk) {
     return key * CH + (chunk ^ (DH == 128 ? key & 15 : (key >> 1) & 7));
   }
@@ -93,7 +94,8 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
   const int outer = w0 >= rows ? 0 : a.tree ? len : s.past + (min(w0 + 32, rows) - 1) / a.group + 1;
 
   f32x16 o[DT];
-  float m = -INFINITY, l = 0.f;
+  float ref = 0.f, l = 0.f;              // weights are 2^(score - ref)
+  float most = -INFINITY;                // what a score may exceed ref by: nothing before the first, then 8
 #pragma unroll
   for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -146,7 +148,7 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
 #pragma unroll
       for (int i = 0; i < SC; ++i) {
         const uint32_t idx = threadIdx.x + i * THREADS, blk = (idx >> 6) % NB;
-        if (SCALES % THREADS == 0 || idx < SCALES)
+        if (idx < SCALES)
           sc[i] = block_scale_load(idx < NB * 64 ? a.c.k_scales : a.c.v_scales, scale0 + (blk << shift) + place + (idx & 63), S16);
       }
       return;
@@ -164,7 +166,7 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
 #pragma unroll
     for (int i = 0; i < SC; ++i) {
       const int idx = threadIdx.x + i * THREADS, key = idx & 63, blk = (idx >> 6) % NB, place = min(j0 + key, last16 + 15) & P1;
-      if (SCALES % THREADS == 0 || idx < SCALES)
+      if (idx < SCALES)
         sc[i] = block_scale_load(idx < NB * 64 ? a.c.k_scales : a.c.v_scales,
                                  scales_at<DH>(a.c, pick(pg, key >> 4), g) + (blk << shift) + place, S16);
     }
@@ -188,14 +190,21 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
 #pragma unroll
     for (int i = 0; i < SC; ++i) {
       const int idx = threadIdx.x + i * THREADS, key = idx & 63, blk = (idx >> 6) % NB;
-      if (idx < NB * 64) st.ks[blk][key] = sc[i] * factor;
-      else if (SCALES % THREADS == 0 || idx < SCALES) st.vs[blk][key] = sc[i];
+      if (idx < NB * 64) {
+        st.ks[blk][key] = sc[i] * factor;
+      } else if (idx < SCALES) {                             // a wavefront's 64 lanes are the 64 tokens of one block
+        const bool fine = (__float_as_uint(sc[i]) & 0x7FFFFFFFu) < 0x7F800000u;
+        const uint64_t bad = __ballot(!fine);
+        st.vs[blk][key] = fine ? sc[i] : 0.f;
+        if ((key & 31) == 0) st.bad[blk][key >> 5] = (uint32_t)(bad >> key);
+      }
     }
   };
 
   // 32 tokens of a tile: scores, weights, output
   const int k_row = (n & 16) | ((n & 4) << 1) | ((n & 8) >> 1) | (n & 3);       // the token of this lane's row of the keys' operand
   auto half = [&](const St& st, int j0, int kh, uint64_t valid) {
+    const uint32_t bad = st.bad[0][kh] | st.bad[NB - 1][kh];
     f32x16 acc[NB];
 #pragma unroll
     for (int blk = 0; blk < NB; ++blk)
@@ -211,7 +220,8 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
     for (int e = 0; e < 16; e += 4) {
       const int at = 32 * kh + 16 * (e >> 3) + 8 * lh + (e & 4);
       const float4 k0 = *reinterpret_cast<const float4*>(&st.ks[0][at]);
-      p[e] = acc[0][e] * k0.x; p[e + 1] = acc[0][e + 1] * k0.y; p[e + 2] = acc[0][e + 2] * k0.z; p[e + 3] = acc[0][e + 3] * k0.w;
+      p[e] = fmaf(acc[0][e], k0.x, -ref); p[e + 1] = fmaf(acc[0][e + 1], k0.y, -ref);
+      p[e + 2] = fmaf(acc[0][e + 2], k0.z, -ref); p[e + 3] = fmaf(acc[0][e + 3], k0.w, -ref);
       if constexpr (NB == 2) {
         const float4 k1 = *reinterpret_cast<const float4*>(&st.ks[NB - 1][at]);
         p[e] = fmaf(acc[NB - 1][e], k1.x, p[e]); p[e + 1] = fmaf(acc[NB - 1][e + 1], k1.y, p[e + 1]);
@@ -234,21 +244,29 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
     float top = fmaxf(p[0], p[1]);
 #pragma unroll
     for (int e = 2; e < 16; ++e) top = fmaxf(top, p[e]);
-    if (__ballot(top > m + 8.0f)) {
+    if (__ballot(top > most)) {
       top = fmaxf(top, __shfl_xor(top, 32, 64));
-      const float mn = fmaxf(m, top);
-      const float keep = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
-      m = mn;
-      l *= keep;
+      if (top > -INFINITY) {
+        const bool fresh = most == -INFINITY;
+        const float next = fresh ? top : ref + fmaxf(top, 0.f), up = next - ref;
+        const float keep = fresh ? 1.f : __builtin_amdgcn_exp2f(-up);        // fresh: there is nothing yet
+        ref = next;
+        most = 8.0f;
+        l *= keep;
 #pragma unroll
-      for (int d = 0; d < DT; ++d) o[d] *= keep;
+        for (int d = 0; d < DT; ++d) o[d] *= keep;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) p[e] -= up;
+      }
     }
-    const float ref = m == -INFINITY ? 0.f : m;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      p[e] = __builtin_amdgcn_exp2f(p[e] - ref);
+      p[e] = __builtin_amdgcn_exp2f(p[e]);
       l += p[e];
     }
+    // a value that is infinite or none goes to all of the rows that see it, and to no others
+    if (__builtin_amdgcn_readfirstlane(bad))
+      if (sees & (bad >> (8 * lh)) & 0x00FF00FFu) l = __uint_as_float(0x7FC00000u);
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
       bf16x8 pf[NB];
@@ -256,13 +274,9 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
       for (int blk = 0; blk < NB; ++blk) {
         const float4 s0 = *reinterpret_cast<const float4*>(&st.vs[blk][32 * kh + 16 * c + 8 * lh]);
         const float4 s1 = *reinterpret_cast<const float4*>(&st.vs[blk][32 * kh + 16 * c + 8 * lh + 4]);
-        float w[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          w[e] *= p[8 * c + e];
-          if (!whole && !((sees >> (16 * c + e)) & 1)) w[e] = 0.f;     // the scale of a token that is not seen may be no number
-        }
-        pf[blk] = __builtin_bit_cast(bf16x8, make_uint4(pack2(w[0], w[1]), pack2(w[2], w[3]), pack2(w[4], w[5]), pack2(w[6], w[7])));
+        const float* w = p + 8 * c;
+        pf[blk] = __builtin_bit_cast(bf16x8, make_uint4(pack2(w[0] * s0.x, w[1] * s0.y), pack2(w[2] * s0.z, w[3] * s0.w),
+                                                        pack2(w[4] * s1.x, w[5] * s1.y), pack2(w[6] * s1.z, w[7] * s1.w)));
       }
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
@@ -302,6 +316,7 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
   }
 
   l += __shfl_xor(l, 32, 64);
+  float m = most == -INFINITY ? -INFINITY : ref;
   if constexpr (KW == 2) {                                   // the second half's results through LDS: [row wavefront][register][lane]
     float* other = reinterpret_cast<float*>(lds) + row_wave * (DT * 16 + 2) * 64 + lane;
     if (key_wave == 1) {

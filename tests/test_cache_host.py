@@ -153,7 +153,7 @@ def test_head_logits_refuse(lib):
     assert call(n=10) == WORKSPACE
 
 
-def test_binding_checks_tensors():
+def test_binding_checks_tensors(monkeypatch):
     """Shapes and types that the C side cannot see are refused by the binding."""
     cfg = config()
     make = lambda c: sw.Cache(c, **{n: torch.zeros(s, dtype=d) for n, (s, d) in c.shapes().items()})  # noqa: E731
@@ -166,27 +166,33 @@ def test_binding_checks_tensors():
     k = torch.zeros((6, 256), dtype=torch.bfloat16)
     q = torch.zeros((6, 512), dtype=torch.bfloat16)
     ok = (cfg, cache, table, past, None, 3)
-    for bad in ((cfg, cache, table.long(), past, None, 3, k, k), (cfg, cache, table[:, :4].contiguous(), past, None, 3, k, k),
-                (cfg, cache, table, past[:1], None, 3, k, k), (cfg, cache, table, past, past.float(), 3, k, k),
-                (cfg, cache, table, past, None, 4, k, k), ok + (k.float(), k), ok + (k[:, :128], k),
-                ok + (k, torch.zeros((6, 300), dtype=torch.bfloat16)[:, :256]), (cfg, make(config(n_pages=9)), table, past, None, 3, k, k)):
-        with pytest.raises((ValueError, TypeError)):
-            sw.swarm_cache_append(*bad)
-    for bad in ((k, k), (k.float(), k), (k[:5], k)):
-        with pytest.raises((ValueError, TypeError)):
-            sw.swarm_cache_read(cfg, cache, table, past, None, 4, *bad)
-    with pytest.raises((ValueError, TypeError)):
-        sw.swarm_cache_keep(cfg, cache, table, past, torch.zeros((2, 2), dtype=torch.int32), past, 3)
-    for other in (dict(tree=torch.zeros((2, 3), dtype=torch.int32)), dict(tree=torch.zeros((2, 2), dtype=torch.int64))):
-        with pytest.raises((ValueError, TypeError)):
-            sw.swarm_cache_attention(*ok, q, q.clone(), None, **other)
-    with pytest.raises(ValueError):
-        sw.swarm_cache_attention(*ok, q, q.clone().t().contiguous().t(), None)
-    with pytest.raises(TypeError):
-        sw.LogitsRules(2, 100, history=torch.zeros((2, 3)), history_len=past)
-    with pytest.raises(ValueError):
-        sw.LogitsRules(2, 100, allowed=torch.zeros((2, 3), dtype=torch.int32))
-    with pytest.raises((ValueError, TypeError)):
-        sw.swarm_logits_adjust(sw.LogitsRules(2, 100), torch.zeros((2, 99)), torch.zeros((2, 100)))
-    with pytest.raises((ValueError, TypeError)):
-        sw.swarm_logits_adjust(sw.LogitsRules(2, 100), torch.zeros((2, 100)), torch.zeros((2, 100), dtype=torch.bfloat16))
+    append, attention = sw.swarm_cache_append, sw.swarm_cache_attention
+    wide = torch.zeros((6, 300), dtype=torch.bfloat16)[:, :256]
+    for why, call in [
+            ("page_table must be", lambda: append(cfg, cache, table.long(), past, None, 3, k, k)),
+            ("page_table has 8 elements", lambda: append(cfg, cache, table[:, :4].contiguous(), past, None, 3, k, k)),
+            ("past has 1 elements", lambda: append(cfg, cache, table, past[:1], None, 3, k, k)),
+            ("fresh must be", lambda: append(cfg, cache, table, past, past.float(), 3, k, k)),
+            ("k has shape", lambda: append(cfg, cache, table, past, None, 4, k, k)),
+            ("k must be", lambda: append(*ok, k.float(), k)),
+            ("k has shape", lambda: append(*ok, k[:, :128], k)),
+            ("same row pitch", lambda: append(*ok, k, wide)),
+            ("another configuration", lambda: append(cfg, make(config(n_pages=9)), table, past, None, 3, k, k)),
+            ("not on the current GPU", lambda: append(*ok, k, k)),
+            ("k_out has", lambda: sw.swarm_cache_read(cfg, cache, table, past, None, 4, k, k)),
+            ("k_out must be", lambda: sw.swarm_cache_read(cfg, cache, table, past, None, 3, k.float(), k)),
+            ("kept has 4 elements", lambda: sw.swarm_cache_keep(cfg, cache, table, past, torch.zeros((2, 2), dtype=torch.int32), past, 3)),
+            ("tree must be", lambda: attention(*ok, q, q.clone(), None, tree=torch.zeros((2, 3), dtype=torch.int32))),
+            ("tree has 4 elements", lambda: attention(*ok, q, q.clone(), None, tree=torch.zeros((2, 2), dtype=torch.int64))),
+            ("out must be contiguous|elements of a row of out", lambda: attention(*ok, q, q.clone().t().contiguous().t(), None)),
+            ("another configuration", lambda: attention(cfg, make(config(page_tokens=32)), table, past, None, 3, q, q.clone(), None)),
+            ("history must be", lambda: sw.LogitsRules(2, 100, history=torch.zeros((2, 3)), history_len=past)),
+            ("allowed has shape", lambda: sw.LogitsRules(2, 100, allowed=torch.zeros((2, 3), dtype=torch.int32))),
+            ("vocab or more", lambda: sw.swarm_logits_adjust(sw.LogitsRules(2, 100), torch.zeros((2, 99)), torch.zeros((2, 100)))),
+            ("out must be", lambda: sw.swarm_logits_adjust(sw.LogitsRules(2, 100), torch.zeros((2, 100)),
+                                                           torch.zeros((2, 100), dtype=torch.bfloat16)))]:
+        with monkeypatch.context() as m:
+            if why != "not on the current GPU":
+                m.setattr(binding, "_device", lambda: -1)               # as if the tensors' device, the CPU, were the current one
+            with pytest.raises((ValueError, TypeError), match=why):
+                call()
