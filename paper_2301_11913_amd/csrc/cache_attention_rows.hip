@@ -54,7 +54,8 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
   constexpr int THREADS = 64 * RW * KW;
   constexpr int NB = DH / 64, DT = DH / 32, KK = DH / 16, Q = 32 * RW;
   constexpr int PIECES = 64 * DH / 16 / THREADS;           // pieces of 16 codes per thread, of keys and of values
-  constexpr int SCALES = 2 * NB * 64, SC = (SCALES + THREADS - 1) / THREADS;
+  constexpr int SCALES = 2 * NB * 64;
+  static_assert(SCALES <= THREADS, "a thread holds one scale of a tile");
   extern __shared__ __attribute__((aligned(16))) char lds[];
   St* stage = reinterpret_cast<St*>(lds);
   const int lane = threadIdx.x & 63, n = lane & 31, lh = lane >> 5;
@@ -104,18 +105,17 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
   // ---- staging: codes and scales of a tile in registers, then bf16 in LDS
   const int shift = a.c.page_shift, P1 = (1 << shift) - 1, last16 = (len - 1) & ~15;
   const int32_t* table = a.c.table + (size_t)b * a.c.table_pages;
-  struct Pages { int p[4]; };                                // of a tile's four times 16 tokens; past the end the last ones
+  // Pages of a tile's four times 16 tokens, past the end the last ones; as they stand in the table, and looked at a tile later, so that
+  // nothing waits for them.
+  struct Pages { int p[4]; };
+  auto is_page = [&](int p) { return (unsigned)p < (unsigned)a.c.n_pages; };
   auto pages_of = [&](int tile) {
     Pages out;
     if (shift >= 6) {
-      const int p = table[(tile * kAttnTile) >> shift];
-      out.p[0] = out.p[1] = out.p[2] = out.p[3] = (unsigned)p < (unsigned)a.c.n_pages ? p : -1;
+      out.p[0] = out.p[1] = out.p[2] = out.p[3] = table[(tile * kAttnTile) >> shift];
     } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int p = table[min(tile * kAttnTile + 16 * i, last16) >> shift];
-        out.p[i] = (unsigned)p < (unsigned)a.c.n_pages ? p : -1;
-      }
+      for (int i = 0; i < 4; ++i) out.p[i] = table[min(tile * kAttnTile + 16 * i, last16) >> shift];
     }
     return out;
   };
@@ -124,52 +124,51 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
     uint64_t v = left >= 64 ? ~0ull : (1ull << left) - 1;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      if (pg.p[i] < 0) v &= ~(0xFFFFull << (16 * i));
+      if (!is_page(pg.p[i])) v &= ~(0xFFFFull << (16 * i));
     return v;
   };
-  auto pick = [&](const Pages& pg, int i) { return max(i == 0 ? pg.p[0] : i == 1 ? pg.p[1] : i == 2 ? pg.p[2] : pg.p[3], 0); };
+  auto pick = [&](const Pages& pg, int i) {
+    const int p = i == 0 ? pg.p[0] : i == 1 ? pg.p[1] : i == 2 ? pg.p[2] : pg.p[3];
+    return is_page(p) ? p : 0;
+  };
   uint4 kc[PIECES], vc[PIECES];
-  float sc[SC];
+  float sc;
   constexpr int KP = DH / 16;                                // pieces of a key row
+  // The addresses first and one set of loads for both cases: with loads in the branches the merge would wait for them.
   auto load = [&](int tile, const Pages& pg) {
     const int j0 = tile * kAttnTile;
+    size_t k_from[PIECES], v_from[PIECES], s_from;
     if (shift >= 6) {                                        // one page: its start is the same for all threads
-      const size_t page0 = codes_at<DH>(a.c, max(pg.p[0], 0), g), scale0 = scales_at<DH>(a.c, max(pg.p[0], 0), g);
+      const size_t page0 = codes_at<DH>(a.c, pick(pg, 0), g), scale0 = scales_at<DH>(a.c, pick(pg, 0), g);
       const int place = j0 & P1;                             // the rest of the page is there, whether written or not
-      const int8_t* k0 = a.c.k_codes + page0 + (size_t)place * DH;
-      const int8_t* v0 = a.c.v_codes + page0 + place;
+      const size_t k0 = page0 + (size_t)place * DH, v0 = page0 + place;
 #pragma unroll
-      for (int i = 0; i < PIECES; ++i) kc[i] = *reinterpret_cast<const uint4*>(k0 + (threadIdx.x + i * THREADS) * 16);
+      for (int i = 0; i < PIECES; ++i) k_from[i] = k0 + (threadIdx.x + i * THREADS) * 16;
 #pragma unroll
       for (int i = 0; i < PIECES; ++i) {
         const uint32_t idx = threadIdx.x + i * THREADS;
-        vc[i] = *reinterpret_cast<const uint4*>(v0 + (((idx >> 2) << shift) + (idx & 3) * 16));
+        v_from[i] = v0 + (((idx >> 2) << shift) + (idx & 3) * 16);
+      }
+      s_from = scale0 + (((threadIdx.x >> 6) % NB) << shift) + place + (threadIdx.x & 63);
+    } else {
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) {
+        const int idx = threadIdx.x + i * THREADS, key = idx / KP, piece = idx % KP, place = min(j0 + key, last16 + 15) & P1;
+        k_from[i] = codes_at<DH>(a.c, pick(pg, key >> 4), g) + place * DH + piece * 16;
       }
 #pragma unroll
-      for (int i = 0; i < SC; ++i) {
-        const uint32_t idx = threadIdx.x + i * THREADS, blk = (idx >> 6) % NB;
-        if (idx < SCALES)
-          sc[i] = block_scale_load(idx < NB * 64 ? a.c.k_scales : a.c.v_scales, scale0 + (blk << shift) + place + (idx & 63), S16);
+      for (int i = 0; i < PIECES; ++i) {
+        const int idx = threadIdx.x + i * THREADS, d = idx >> 2, piece = idx & 3, place = min(j0 + piece * 16, last16) & P1;
+        v_from[i] = codes_at<DH>(a.c, pick(pg, piece), g) + (d << shift) + place;
       }
-      return;
+      const int key = threadIdx.x & 63, blk = (threadIdx.x >> 6) % NB, place = min(j0 + key, last16 + 15) & P1;
+      s_from = scales_at<DH>(a.c, pick(pg, key >> 4), g) + (blk << shift) + place;
     }
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-      const int idx = threadIdx.x + i * THREADS, key = idx / KP, piece = idx % KP, place = min(j0 + key, last16 + 15) & P1;
-      kc[i] = *reinterpret_cast<const uint4*>(a.c.k_codes + codes_at<DH>(a.c, pick(pg, key >> 4), g) + place * DH + piece * 16);
-    }
+    for (int i = 0; i < PIECES; ++i) kc[i] = *reinterpret_cast<const uint4*>(a.c.k_codes + k_from[i]);
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-      const int idx = threadIdx.x + i * THREADS, d = idx >> 2, piece = idx & 3, place = min(j0 + piece * 16, last16) & P1;
-      vc[i] = *reinterpret_cast<const uint4*>(a.c.v_codes + codes_at<DH>(a.c, pick(pg, piece), g) + (d << shift) + place);
-    }
-#pragma unroll
-    for (int i = 0; i < SC; ++i) {
-      const int idx = threadIdx.x + i * THREADS, key = idx & 63, blk = (idx >> 6) % NB, place = min(j0 + key, last16 + 15) & P1;
-      if (idx < SCALES)
-        sc[i] = block_scale_load(idx < NB * 64 ? a.c.k_scales : a.c.v_scales,
-                                 scales_at<DH>(a.c, pick(pg, key >> 4), g) + (blk << shift) + place, S16);
-    }
+    for (int i = 0; i < PIECES; ++i) vc[i] = *reinterpret_cast<const uint4*>(a.c.v_codes + v_from[i]);
+    sc = block_scale_load(wave < NB ? a.c.k_scales : a.c.v_scales, s_from, S16);              // of threads beyond SCALES: in bounds, of no use
   };
   const float factor = (DH == 64 ? 0.125f : 0.08838834764831845f) * kLog2e;
   auto store = [&](St& st) {
@@ -187,17 +186,14 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
       st.v[St::v_at(d, 2 * piece)] = make_uint4(w0.x, w0.y, w1.x, w1.y);
       st.v[St::v_at(d, 2 * piece + 1)] = make_uint4(w2.x, w2.y, w3.x, w3.y);
     }
-#pragma unroll
-    for (int i = 0; i < SC; ++i) {
-      const int idx = threadIdx.x + i * THREADS, key = idx & 63, blk = (idx >> 6) % NB;
-      if (idx < NB * 64) {
-        st.ks[blk][key] = sc[i] * factor;
-      } else if (idx < SCALES) {                             // a wavefront's 64 lanes are the 64 tokens of one block
-        const bool fine = (__float_as_uint(sc[i]) & 0x7FFFFFFFu) < 0x7F800000u;
-        const uint64_t bad = __ballot(!fine);
-        st.vs[blk][key] = fine ? sc[i] : 0.f;
-        if ((key & 31) == 0) st.bad[blk][key >> 5] = (uint32_t)(bad >> key);
-      }
+    const int key = threadIdx.x & 63, blk = wave % NB;       // a wavefront's 64 lanes are the 64 tokens of one block
+    if (wave < NB) {
+      st.ks[blk][key] = sc * factor;
+    } else if (wave < 2 * NB) {
+      const bool fine = (__float_as_uint(sc) & 0x7FFFFFFFu) < 0x7F800000u;
+      const uint64_t bad = __ballot(!fine);
+      st.vs[blk][key] = fine ? sc : 0.f;
+      if ((key & 31) == 0) st.bad[blk][key >> 5] = (uint32_t)(bad >> key);
     }
   };
 
