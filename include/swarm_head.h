@@ -81,7 +81,7 @@ swarm_status swarm_head_logits(const swarm_head_config *cfg, const swarm_head_pa
  * history [rows, history_max], bias_ids and bias [rows, bias_max], allowed [rows, ceil(vocab / 32)] are device arrays; history,
  * bias_ids and allowed may be NULL (no such rule), and so may repetition (1), frequency (0) and presence (0).  Ids outside
  * [0, vocab) are ignored; a length outside 0 .. its maximum counts as the nearer end.
- * 1 <= rows <= 65535; 1 <= vocab <= 2^24; 0 <= history_max <= 2^24; 0 <= bias_max <= 1024; pitches >= vocab. */
+ * 1 <= rows <= 65535; 1 <= vocab <= 2^24; 0 <= history_max < 2^20; 0 <= bias_max <= 1024; pitches >= vocab. */
 typedef struct {
   int32_t rows, vocab;
   int32_t history_max, bias_max;

@@ -24,6 +24,8 @@ typedef __attribute__((ext_vector_type(2))) float f32x2;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 
 constexpr float kLog2e = 1.4426950408889634f;
+// 4 prompts of 2048 tokens, 32 heads of 128: 222 us; 4 pairs at a time 225, 2 241, one 262, all 16 of an XCD 221
+constexpr int kPairs = 8;
 
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
   f32x2 v = {a, b};
@@ -61,12 +63,13 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
   const int lane = threadIdx.x & 63, n = lane & 31, lh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row_wave = wave % RW, key_wave = wave / RW;
-  // workgroups go to the 8 XCDs in turn: all units of a sequence and head to one, which keeps its tiles in that XCD's L2; the last
-  // rows, which see the most, first
-  const int per_pair = a.row_groups * a.splits, x = blockIdx.x >> 3;
-  const int pair = x / per_pair * 8 + (blockIdx.x & 7);
+  // Workgroups go to the 8 XCDs in turn: all units of a sequence and head to one, kPairs of these at a time, so that its L2 holds what
+  // they read; among them the last rows, which see the most, first.
+  const int per_pair = a.row_groups * a.splits, mine = (a.c.B * a.c.KV + 7) >> 3, x = blockIdx.x >> 3;
+  const int turn = x / (kPairs * per_pair), left = x - turn * kPairs * per_pair, width = min(kPairs, mine - turn * kPairs);
+  const int which = left / width, pair = (turn * kPairs + left % width) * 8 + (blockIdx.x & 7);
   if (pair >= a.c.B * a.c.KV) return;
-  const int which = x % per_pair, rg = a.row_groups - 1 - which / a.splits, split = which % a.splits;
+  const int rg = a.row_groups - 1 - which / a.splits, split = which % a.splits;
   const int b = pair / a.c.KV, g = pair - b * a.c.KV;
   const Span s = span_of(a.c, b);
   const int r0 = rg * Q, rows = s.fresh * a.group;

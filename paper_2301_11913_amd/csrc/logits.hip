@@ -1,9 +1,9 @@
 // Rules on rows of logits: penalties for tokens that a row's history holds, biases, a mask of allowed tokens.
 //
-// One pass over the logits.  A workgroup owns kColumns columns of one row: it counts the history's tokens that fall among them in
-// LDS (whole numbers, so the order of the additions does not matter), adds up the biases that do, and then rewrites its columns.  The
-// history is read by every workgroup of the row (from cache: 8 KB for 2048 tokens), which costs less than a pass of its own over
-// the logits to mark it.
+// One pass over the logits.  A workgroup owns kColumns columns of one row: it asks for its logits, counts the history's tokens that fall
+// among them in LDS (whole numbers, so the order of the additions does not matter) and adds up the biases that do, and then writes its
+// columns, four to a thread at a time; most have neither, and a look at their four words in LDS is all that costs.  The history is read by every
+// workgroup of the row (from cache: 8 KB for 2048 tokens), which costs less than a pass of its own over the logits to mark it.
 #include "kernels.h"
 #include "swarm_head.h"
 
@@ -11,8 +11,12 @@ namespace swarm {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kColumns = 2048;
+constexpr int kColumns = 4096;
+constexpr int kSteps = kColumns / (4 * kThreads);      // groups of four columns per thread
 constexpr int kMaxBias = 1024;
+// a column's word in LDS: a bias, more than one, which entry of the row's list (10 bits), and how often the history has it
+constexpr uint32_t kBiased = 0x80000000u, kTwice = 0x40000000u, kEntry = 0x3FF00000u, kCount = 0x000FFFFFu;
+constexpr int kEntryShift = 20;
 
 struct LogitsArgs {
   swarm_logits_rules r;
@@ -21,52 +25,123 @@ struct LogitsArgs {
   size_t pitch, out_pitch;
 };
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void logits_adjust_kernel(LogitsArgs a) {
-  __shared__ int count[kColumns];
-  __shared__ float bias[kColumns];
-  __shared__ uint32_t biased[kColumns / 32];
-  const int row = blockIdx.y, c0 = blockIdx.x * kColumns, n = min(kColumns, a.r.vocab - c0);
-  const int said = a.r.history ? min(max(a.r.history_len[row], 0), a.r.history_max) : 0;
-  const int given = a.r.bias_ids ? min(max(a.r.bias_len[row], 0), a.r.bias_max) : 0;
-  for (int i = threadIdx.x; i < kColumns; i += kThreads) count[i] = 0;
-  if (threadIdx.x < kColumns / 32) biased[threadIdx.x] = 0;
-  __syncthreads();
-  const int32_t* history = a.r.history + (size_t)row * a.r.history_max;
-  for (int i = threadIdx.x; i < said; i += kThreads) {
-    const int v = history[i] - c0;
-    if ((unsigned)v < (unsigned)n) atomicAdd(&count[v], 1);
-  }
-  const int32_t* ids = a.r.bias_ids + (size_t)row * a.r.bias_max;
-  for (int i = threadIdx.x; i < given; i += kThreads) {
-    const int id = ids[i], v = id - c0;
-    if ((unsigned)v >= (unsigned)n) continue;
-    bool first = true;                    // the first entry of an id adds up all of them, in order
-    for (int e = 0; e < i; ++e) first &= ids[e] != id;
-    if (!first) continue;
-    float sum = 0.0f;
-    for (int e = i; e < given; ++e)
-      if (ids[e] == id) sum += a.r.bias[(size_t)row * a.r.bias_max + e];
-    bias[v] = sum;
-    atomicOr(&biased[v >> 5], 1u << (v & 31));
-  }
-  __syncthreads();
-  const float rep = a.r.repetition ? a.r.repetition[row] : 1.0f;
-  const float freq = a.r.frequency ? a.r.frequency[row] : 0.0f, pres = a.r.presence ? a.r.presence[row] : 0.0f;
+// four values of a row that starts anywhere
+struct __attribute__((packed, aligned(4))) Floats4 { float v[4]; };
+struct __attribute__((packed, aligned(2))) Halves4 { uint16_t v[4]; };
+__device__ __forceinline__ void load4(const float* p, float (&x)[4]) {
+  const Floats4 w = *reinterpret_cast<const Floats4*>(p);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = w.v[i];
+}
+__device__ __forceinline__ void load4(const bf16_raw* p, float (&x)[4]) {
+  const Halves4 w = *reinterpret_cast<const Halves4*>(p);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = bf16_bits_to_float(w.v[i]);
+}
+
+// WHOLE: kColumns columns and no fewer
+template <typename T, bool WHOLE>
+__device__ __forceinline__ void adjust_columns(const LogitsArgs& a, int row, int c0, uint4* words, float* bias) {
+  uint32_t* word = reinterpret_cast<uint32_t*>(words);
+  const int n = WHOLE ? kColumns : a.r.vocab - c0;
   const T* in = reinterpret_cast<const T*>(a.logits) + (size_t)row * a.pitch + c0;
   float* out = a.out + (size_t)row * a.out_pitch + c0;
-  const uint32_t* allowed = a.r.allowed ? a.r.allowed + (size_t)row * ((a.r.vocab + 31) >> 5) + (c0 >> 5) : nullptr;
-  for (int i = threadIdx.x; i < n; i += kThreads) {
-    float x = Elem<T>::load(in + i);
-    const int times = count[i];
-    if (times > 0) {
-      x = x > 0.0f ? x / rep : x * rep;
-      x = x - freq * (float)times - pres;
+  float x[kSteps][4];
+  uint32_t allowed[kSteps];
+#pragma unroll
+  for (int s = 0; s < kSteps; ++s) {
+    const int c = (s * kThreads + threadIdx.x) * 4;
+    if constexpr (WHOLE) {
+      load4(in + c, x[s]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[s][i] = c + i < n ? Elem<T>::load(in + c + i) : 0.0f;
     }
-    if ((biased[i >> 5] >> (i & 31)) & 1) x += bias[i];
-    if (allowed && !((allowed[i >> 5] >> (i & 31)) & 1)) x = -INFINITY;
-    out[i] = x;
+    allowed[s] = 0xF;
+    if (a.r.allowed && c < n) allowed[s] = a.r.allowed[(size_t)row * ((a.r.vocab + 31) >> 5) + ((c0 + c) >> 5)] >> (c & 31);
   }
+  const float rep = a.r.repetition ? a.r.repetition[row] : 1.0f;
+  const float freq = a.r.frequency ? a.r.frequency[row] : 0.0f, pres = a.r.presence ? a.r.presence[row] : 0.0f;
+  const int said = a.r.history ? min(max(a.r.history_len[row], 0), a.r.history_max) : 0;
+  const int given = a.r.bias_ids ? min(max(a.r.bias_len[row], 0), a.r.bias_max) : 0;
+#pragma unroll
+  for (int s = 0; s < kSteps; ++s) words[s * kThreads + threadIdx.x] = make_uint4(0, 0, 0, 0);
+  __syncthreads();
+  const int32_t* history = a.r.history + (size_t)row * a.r.history_max;
+#pragma unroll 8
+  for (int i = threadIdx.x; i < said; i += kThreads) {
+    const int v = history[i] - c0;
+    if ((unsigned)v < (unsigned)n) atomicAdd(&word[v], 1u);
+  }
+  const int32_t* ids = a.r.bias_ids + (size_t)row * a.r.bias_max;
+  const float* biases = a.r.bias + (size_t)row * a.r.bias_max;
+  for (int i = threadIdx.x; i < given; i += kThreads) {
+    const int v = ids[i] - c0;
+    if ((unsigned)v >= (unsigned)n) continue;
+    bias[i] = biases[i];
+    if (atomicOr(&word[v], kBiased | (uint32_t)i << kEntryShift) & kBiased) atomicOr(&word[v], kTwice);
+  }
+  __syncthreads();
+  bool twice = false;
+  for (int i = threadIdx.x; i < given; i += kThreads) {
+    const int v = ids[i] - c0;
+    twice |= (unsigned)v < (unsigned)n && (word[v] & kTwice);
+  }
+  if (__syncthreads_or(twice)) {
+    for (int i = threadIdx.x; i < given; i += kThreads) {
+      const int id = ids[i], v = id - c0;
+      if ((unsigned)v >= (unsigned)n || !(word[v] & kTwice)) continue;
+      bool first = true;                  // the first entry of an id adds up all of them, in order, and is the one that counts
+      for (int e = 0; e < i; ++e) first &= ids[e] != id;
+      if (!first) continue;
+      float sum = 0.0f;
+      for (int e = i; e < given; ++e)
+        if (ids[e] == id) sum += biases[e];
+      bias[i] = sum;
+      word[v] = (word[v] & ~kEntry) | (uint32_t)i << kEntryShift;
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int s = 0; s < kSteps; ++s) {
+    const int c = (s * kThreads + threadIdx.x) * 4;
+    if (c >= n) break;
+    const uint4 w4 = words[s * kThreads + threadIdx.x];
+    const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
+    if (w[0] | w[1] | w[2] | w[3]) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t times = w[i] & kCount;
+        if (times) {
+          x[s][i] = x[s][i] > 0.0f ? x[s][i] / rep : x[s][i] * rep;
+          x[s][i] = x[s][i] - freq * (float)times - pres;
+        }
+        if (w[i] & kBiased) x[s][i] += bias[(w[i] & kEntry) >> kEntryShift];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (!((allowed[s] >> i) & 1)) x[s][i] = -INFINITY;
+    if constexpr (WHOLE) {
+      Floats4 y;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y.v[i] = x[s][i];
+      *reinterpret_cast<Floats4*>(out + c) = y;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (c + i < n) out[c + i] = x[s][i];
+    }
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void logits_adjust_kernel(LogitsArgs a) {
+  __shared__ uint4 words[kColumns / 4];
+  __shared__ float bias[kMaxBias];
+  const int row = blockIdx.y, c0 = blockIdx.x * kColumns;
+  if (a.r.vocab - c0 >= kColumns) adjust_columns<T, true>(a, row, c0, words, bias);
+  else adjust_columns<T, false>(a, row, c0, words, bias);
 }
 
 }  // namespace
@@ -80,7 +155,7 @@ extern "C" swarm_status swarm_logits_adjust(const swarm_logits_rules* r, const v
   if ((r->history && !r->history_len) || (r->bias_ids && (!r->bias || !r->bias_len))) return SWARM_ERR_NULL;
   if (dtype != SWARM_F32 && dtype != SWARM_BF16) return SWARM_ERR_DTYPE;
   if (r->rows < 1 || r->rows > 65535 || r->vocab < 1 || r->vocab > (1 << 24)) return SWARM_ERR_SHAPE;
-  if (r->history_max < 0 || r->history_max > (1 << 24) || r->bias_max < 0 || r->bias_max > kMaxBias) return SWARM_ERR_SHAPE;
+  if (r->history_max < 0 || r->history_max > (int)kCount || r->bias_max < 0 || r->bias_max > kMaxBias) return SWARM_ERR_SHAPE;
   if (logits_pitch < (size_t)r->vocab || out_pitch < (size_t)r->vocab) return SWARM_ERR_SHAPE;
   if (((uintptr_t)logits & (dtype == SWARM_BF16 ? 1 : 3)) || ((uintptr_t)out & 3)) return SWARM_ERR_SHAPE;
   if (logits == out && (dtype != SWARM_F32 || logits_pitch != out_pitch)) return SWARM_ERR_SHAPE;

@@ -138,7 +138,7 @@ def test_logits_refuse(lib):
     for other in (dict(logits=None), dict(out=None), dict(history_len=None), dict(bias=None), dict(bias_len=None)):
         assert call(**other) == NULL
     assert call(dtype=5) == DTYPE
-    for other in (dict(rows=0), dict(rows=65536), dict(vocab=0), dict(vocab=(1 << 24) + 1), dict(history_max=-1), dict(bias_max=-1),
+    for other in (dict(rows=0), dict(rows=65536), dict(vocab=0), dict(vocab=(1 << 24) + 1), dict(history_max=-1), dict(history_max=1 << 20), dict(bias_max=-1),
                   dict(bias_max=1025), dict(pitch=99), dict(out_pitch=99), dict(logits=A + 1), dict(out=A + 2), dict(out=A)):
         assert call(**other) == SHAPE
     assert call(dtype=0, out=A, out_pitch=101) == SHAPE                   # in place with another pitch
