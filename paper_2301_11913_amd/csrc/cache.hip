@@ -71,39 +71,49 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, int block, doub
     }
     __syncthreads();
   }
-  constexpr int C = DH / 8;
+  // A pass: HS heads of the tile's tokens, one chunk of 8 elements per thread; U passes' loads are on their way together.  Threads beyond
+  // the last token or head do the last one's work over again, without writing it.
+  constexpr int C = DH / 8, HS = kThreads / (kTokens * C), U = 4;
   const int q_heads = ROT ? a.c.H : 0, heads = q_heads + a.c.KV;
   const int h0 = group * a.heads_per_group, h1 = min(heads, h0 + a.heads_per_group);
-  for (int i = threadIdx.x; i < (h1 - h0) * kTokens * C; i += kThreads) {
-    const int chunk = i % C, t = i / C % kTokens, h = h0 + i / (C * kTokens);
-    if (t >= n) continue;
-    const bool is_q = h < q_heads;
-    const int head = is_q ? h : h - q_heads;
-    const T* src = reinterpret_cast<const T*>(is_q ? a.q : a.k) + (row0 + t) * a.pitch + (size_t)head * DH + chunk * 8;
-    float x[8];
-    Row8<T>::load(src, x);
-    if constexpr (ROT) {
+  const int chunk = threadIdx.x % C, mine = threadIdx.x / C % kTokens, t = min(mine, n - 1);
+  const int hh = __builtin_amdgcn_readfirstlane(threadIdx.x / (C * kTokens));
+  const int j = s.past + t0 + t, page = page_of(a.c, b, j), place = j & ((1 << a.c.page_shift) - 1);
+  for (int hb = h0 + hh; hb < h1; hb += U * HS) {
+    float x[U][8];
 #pragma unroll
-      for (int p = 0; p < 4; ++p) {
-        const double2 w = turn[t * (DH / 2) + chunk * 4 + p];
-        const double e = x[2 * p], o = x[2 * p + 1];
-        x[2 * p] = (float)(e * w.x - o * w.y);
-        x[2 * p + 1] = (float)(e * w.y + o * w.x);
-      }
-      if (is_q) {
-        Row8<T>::store(reinterpret_cast<T*>(a.q_out) + (row0 + t) * a.q_out_pitch + (size_t)head * DH + chunk * 8, x);
-        continue;
-      }
+    for (int u = 0; u < U; ++u) {
+      const int h = min(hb + u * HS, h1 - 1);
+      const T* src = reinterpret_cast<const T*>(h < q_heads ? a.q : a.k) + (row0 + t) * a.pitch + (size_t)(h < q_heads ? h : h - q_heads) * DH;
+      Row8<T>::load(src + chunk * 8, x[u]);
     }
-    int c[8];
-    const float scale = encode8(x, c, a.s16);
-    const int j = s.past + t0 + t, page = page_of(a.c, b, j);
-    if (page < 0) continue;
-    const int place = j & ((1 << a.c.page_shift) - 1);
-    *reinterpret_cast<uint2*>(a.c.k_codes + codes_at<DH>(a.c, page, head) + (size_t)place * DH + chunk * 8) =
-        make_uint2(bytes4(c[0], c[1], c[2], c[3]), bytes4(c[4], c[5], c[6], c[7]));
-    if ((chunk & 7) == 0)
-      block_scale_store(a.c.k_scales, scales_at<DH>(a.c, page, head) + ((size_t)(chunk >> 3) << a.c.page_shift) + place, scale, a.s16);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int h = hb + u * HS;
+      if (h >= h1) break;
+      const bool is_q = h < q_heads;
+      const int head = is_q ? h : h - q_heads;
+      if constexpr (ROT) {
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          const double2 w = turn[t * (DH / 2) + chunk * 4 + p];
+          const double e = x[u][2 * p], o = x[u][2 * p + 1];
+          x[u][2 * p] = (float)(e * w.x - o * w.y);
+          x[u][2 * p + 1] = (float)(e * w.y + o * w.x);
+        }
+        if (is_q) {
+          if (mine < n) Row8<T>::store(reinterpret_cast<T*>(a.q_out) + (row0 + t) * a.q_out_pitch + (size_t)head * DH + chunk * 8, x[u]);
+          continue;
+        }
+      }
+      int c[8];
+      const float scale = encode8(x[u], c, a.s16);
+      if (mine >= n || page < 0) continue;
+      *reinterpret_cast<uint2*>(a.c.k_codes + codes_at<DH>(a.c, page, head) + (size_t)place * DH + chunk * 8) =
+          make_uint2(bytes4(c[0], c[1], c[2], c[3]), bytes4(c[4], c[5], c[6], c[7]));
+      if ((chunk & 7) == 0)
+        block_scale_store(a.c.k_scales, scales_at<DH>(a.c, page, head) + ((size_t)(chunk >> 3) << a.c.page_shift) + place, scale, a.s16);
+    }
   }
 }
 
@@ -119,19 +129,23 @@ __device__ __forceinline__ void append_values(const AppendArgs& a, int block, ui
   const int chunk = threadIdx.x % C, quad = threadIdx.x / C;                     // d_head 64: half of the threads have no tokens
   if (quad < kTile / 4) {
     uint32_t words[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    float x[4][8];
+    int pages[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {                  // all loads first; places that are not new take the nearest one that is
+      const int j = min(max(base + quad * 4 + u, s.past), end - 1);
+      Row8<T>::load(reinterpret_cast<const T*>(a.v) + ((size_t)b * a.c.tokens + (j - s.past)) * a.pitch + (size_t)head * DH + chunk * 8, x[u]);
+      pages[u] = page_of(a.c, b, j);
+    }
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const int j = base + quad * 4 + u;
-      if (j < s.past || j >= end) continue;
-      float x[8];
-      Row8<T>::load(reinterpret_cast<const T*>(a.v) + ((size_t)b * a.c.tokens + (j - s.past)) * a.pitch + (size_t)head * DH + chunk * 8, x);
       int c[8];
-      const float scale = encode8(x, c, a.s16);
+      const float scale = encode8(x[u], c, a.s16);
 #pragma unroll
       for (int i = 0; i < 8; ++i) words[i] |= (uint32_t)(c[i] & 0xFF) << (8 * u);
-      const int page = page_of(a.c, b, j);
-      if ((chunk & 7) == 0 && page >= 0)
-        block_scale_store(a.c.v_scales, scales_at<DH>(a.c, page, head) + ((size_t)(chunk >> 3) << a.c.page_shift) +
+      if ((chunk & 7) == 0 && pages[u] >= 0 && j >= s.past && j < end)
+        block_scale_store(a.c.v_scales, scales_at<DH>(a.c, pages[u], head) + ((size_t)(chunk >> 3) << a.c.page_shift) +
                           (j & ((1 << a.c.page_shift) - 1)), scale, a.s16);
     }
 #pragma unroll
