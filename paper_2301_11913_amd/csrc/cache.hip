@@ -262,17 +262,23 @@ __global__ __launch_bounds__(kThreads) void cache_keep_kernel(CacheArgs a, const
   __shared__ uint32_t values[DH * kDraftBytes / 4];
   __shared__ float scales[2][DH / 64][kDraft];
   __shared__ int from[kDraft];
+  __shared__ __attribute__((aligned(16))) uint8_t place_from[80];   // where the value that goes to a place lies among the values read
   const int b = blockIdx.x / a.KV, head = blockIdx.x - b * a.KV;
   const Span s = span_of(a, b);                 // fresh: how many are kept
   if (s.fresh == 0) return;
   const int P1 = (1 << a.page_shift) - 1;
   const long long cap = (long long)a.table_pages << a.page_shift;
-  if ((int)threadIdx.x < s.fresh) {
-    const int u = kept[(size_t)b * a.tokens + threadIdx.x];
-    const bool ok = u >= 0 && u < a.tokens && (long long)s.past + u < cap && page_of(a, b, s.past + u) >= 0;
-    from[threadIdx.x] = ok ? u : -1;
-  }
   const int base = s.past & ~15, off = s.past - base;
+  if (threadIdx.x < 80) {
+    const int j = (int)threadIdx.x - off;
+    int u = -1;
+    if (j >= 0 && j < s.fresh) {
+      u = kept[(size_t)b * a.tokens + j];
+      if (u < 0 || u >= a.tokens || (long long)s.past + u >= cap || page_of(a, b, s.past + u) < 0) u = -1;
+      from[j] = u;
+    }
+    place_from[threadIdx.x] = (uint8_t)(u < 0 ? (int)threadIdx.x : off + u);
+  }
   // places of the draft that the table can hold, in chunks of 16
   const int last = (int)min((long long)s.past + a.tokens, cap), chunks = (last - base + 15) >> 4;
   for (int i = threadIdx.x; i < DH * chunks; i += kThreads) {
@@ -309,18 +315,17 @@ __global__ __launch_bounds__(kThreads) void cache_keep_kernel(CacheArgs a, const
     block_scale_store(what & 1 ? a.v_scales : a.k_scales, scales_at<DH>(a, page, head) + ((size_t)(what >> 1) << a.page_shift) +
                       (at & P1), scales[what & 1][what >> 1][j], s16);
   }
-  const int to_chunks = (off + s.fresh + 15) >> 4;
-  for (int i = threadIdx.x; i < DH * to_chunks; i += kThreads) {
-    const int d = i / to_chunks, c = i - d * to_chunks, j0 = base + 16 * c, page = page_of(a, b, j0);
+  // a chunk of 16 places per wavefront at a time: its sources are the same for all elements
+  const int to_chunks = (off + s.fresh + 15) >> 4, d = threadIdx.x % DH;
+  for (int c = threadIdx.x / DH; c < to_chunks; c += kThreads / DH) {
+    const int j0 = base + 16 * c, page = page_of(a, b, j0);
     if (page < 0) continue;
     const uint8_t* row = reinterpret_cast<const uint8_t*>(values) + d * kDraftBytes;
+    const uint4 at = *reinterpret_cast<const uint4*>(place_from + 16 * c);
+    const uint32_t src[4] = {at.x, at.y, at.z, at.w};
     uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const int j = 16 * c + e - off;
-      const int u = j >= 0 && j < s.fresh ? from[j] : -1;
-      w[e >> 2] |= (uint32_t)row[u < 0 ? 16 * c + e : off + u] << (8 * (e & 3));
-    }
+    for (int e = 0; e < 16; ++e) w[e >> 2] |= (uint32_t)row[(src[e >> 2] >> (8 * (e & 3))) & 0xFF] << (8 * (e & 3));
     *reinterpret_cast<uint4*>(a.v_codes + codes_at<DH>(a, page, head) + ((size_t)d << a.page_shift) + (j0 & P1)) =
         make_uint4(w[0], w[1], w[2], w[3]);
   }
