@@ -98,6 +98,10 @@ inline CacheArgs cache_args(const swarm_cache_config* c, const swarm_cache* k, c
                    __builtin_ctz((unsigned)c->page_tokens), c->n_pages, c->batch, c->table_pages, tokens};
 }
 
+// rows of one key / value head (tokens x query heads of it) that a kernel counts in 32 bits
+inline bool cache_attention_shape_ok(const swarm_cache_config* c, int tokens) {
+  return (long long)tokens * (c->n_heads / c->n_kv_heads) <= (1ll << 24);
+}
 // Attention over a cache (checked arguments); `scratch` holds cache_attention_scratch_bytes of it.
 size_t cache_attention_scratch_bytes(const swarm_cache_config* c, int tokens, int max_len);
 swarm_status cache_attention_launch(const swarm_cache_config* c, const CacheArgs& a, int max_len, const void* q, size_t q_pitch,

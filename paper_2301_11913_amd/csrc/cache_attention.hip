@@ -403,12 +403,15 @@ struct Cut {
 Cut cut_of(const swarm_cache_config* c, int tokens, int max_len) {
   Cut k{};
   const int rows = tokens * (c->n_heads / c->n_kv_heads);
-  k.many = c->dtype == SWARM_BF16 && rows > 16;
+  // bf16, 8 sequences of 4000 tokens, 32 heads, with 4 / 5 / 8 / 16 / 32 rows each: the kernel of bytes 56 / 74 / 75 / 96 / 149 us at
+  // d_head 128 and 32 / - / 34 / 62 / 96 at 64, the kernel of many rows 65 / 65 / 64 / 67 / 69 and 47 / - / 47 / 47 / 49
+  k.many = c->dtype == SWARM_BF16 && rows > (c->d_head == 64 ? 8 : 4);
   if (k.many) {
     k.row_tiles = rows <= 64 ? 2 : 4;
     k.rows = 32 * k.row_tiles;
   } else {
-    k.row_tiles = rows <= 4 ? 1 : rows <= 8 ? 2 : 4;
+    // fp32, the same with 16 heads and 9 / 32 rows: tiles of 8 rows 26 / 37 us at d_head 64 and 68 / 106 at 128, of 16 rows 34 / 53 and 57 / 92
+    k.row_tiles = rows <= 4 ? 1 : rows <= 8 || c->d_head == 64 ? 2 : 4;
     k.rows = 4 * k.row_tiles;
   }
   k.row_groups = (rows + k.rows - 1) / k.rows;
@@ -448,10 +451,11 @@ swarm_status launch(const AttnArgs& a, const Cut& k, hipStream_t st) {
     if (st1 != SWARM_OK) return st1;
   } else if (k.row_tiles == 1) {
     launch_bytes<T, DH, 1>(a, (unsigned)blocks, st);
-  } else if (k.row_tiles == 2) {
-    launch_bytes<T, DH, 2>(a, (unsigned)blocks, st);
   } else {
-    launch_bytes<T, DH, 4>(a, (unsigned)blocks, st);
+    if constexpr (sizeof(T) == 4 || DH == 64)
+      if (k.row_tiles == 2) launch_bytes<T, DH, 2>(a, (unsigned)blocks, st);
+    if constexpr (sizeof(T) == 4 && DH == 128)
+      if (k.row_tiles == 4) launch_bytes<T, DH, 4>(a, (unsigned)blocks, st);
   }
   if (k.splits > 1) {
     int slices = 1024 / DH;
@@ -481,7 +485,7 @@ swarm_status cache_attention_launch(const swarm_cache_config* c, const CacheArgs
 using namespace swarm;
 
 extern "C" size_t swarm_cache_attention_workspace_bytes(const swarm_cache_config* cfg, int32_t tokens, int32_t max_len) {
-  if (cache_config_status(cfg, tokens) != SWARM_OK || max_len < 0) return 0;
+  if (cache_config_status(cfg, tokens) != SWARM_OK || max_len < 0 || !cache_attention_shape_ok(cfg, tokens)) return 0;
   return cache_attention_scratch_bytes(cfg, tokens, max_len);
 }
 
@@ -493,7 +497,7 @@ extern "C" swarm_status swarm_cache_attention(const swarm_cache_config* cfg, con
   const swarm_status bad = cache_config_status(cfg, tokens);
   if (bad != SWARM_OK) return bad;
   const size_t width = (size_t)cfg->n_heads * cfg->d_head;
-  if (max_len < 0 || (tree && tokens > 64) || q == out || !cache_aligned(cache) || !pitch_ok(q, q_pitch, width, cfg->dtype) ||
+  if (max_len < 0 || !cache_attention_shape_ok(cfg, tokens) || (tree && tokens > 64) || q == out || !cache_aligned(cache) || !pitch_ok(q, q_pitch, width, cfg->dtype) ||
       !pitch_ok(out, out_pitch, width, cfg->dtype) || ((uintptr_t)tree & 7) || ((uintptr_t)workspace & 255))
     return SWARM_ERR_SHAPE;
   const size_t need = cache_attention_scratch_bytes(cfg, tokens, max_len);

@@ -64,6 +64,9 @@ def test_dtype_tokens_and_null(lib):
     cfg.c.dtype = 7
     assert all(call() == DTYPE for call in calls(lib, cfg, pool()).values())
     cfg = config()
+    shared = config(n_heads=1024, n_kv_heads=1, batch=1)
+    assert calls(lib, shared, pool(), (1 << 14) + 1, q_pitch=1 << 16, out_pitch=1 << 16)["attention"]() == SHAPE
+    assert sw.swarm_cache_attention_workspace_bytes(shared, (1 << 14) + 1, 80) == 0
     for tokens in (0, -1, (1 << 23) + 1):
         assert all(call() == SHAPE for call in calls(lib, cfg, pool(), tokens).values())
     assert all(call() == NULL for call in calls(lib, cfg, None).values())

@@ -102,6 +102,33 @@ def test_append_rotates(dtype, H, KV, dh, T, past, page, bits, where):
     assert np.array_equal(q.double().cpu().numpy(), got[:, :H * dh])
 
 
+@pytest.mark.parametrize("bits", [32, 16])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_append_is_the_codec(dtype, bits):
+    """Rows of all sizes, infinities and no numbers among them: the bits that swarm_codec_encode gives."""
+    import paper_2301_11913_amd as sw
+    KV, dh, T, page = 3, 128, 40, 16
+    w = World(99, dtype, KV, KV, dh, T, [9], page, bits)
+    cfg, cache = w.upload()
+    x = w.normal(T, KV * dh)
+    x *= 2.0 ** w.rng.integers(-60, 60, (T, 1))
+    x[3, 5], x[4, 70], x[5, :64], x[6, 130] = np.inf, np.nan, -np.inf, -np.inf
+    x[7] *= 2.0 ** -130 / np.abs(x[7]).max()
+    dev = w.dev(x)
+    sw.swarm_cache_append(cfg, cache, w.ints(w.table), w.ints(w.past), None, T, dev, dev)
+    codes = torch.empty(dev.numel(), dtype=torch.int8, device="cuda")
+    scales = torch.empty(dev.numel() // 64, dtype=torch.float32 if bits == 32 else torch.bfloat16, device="cuda")
+    (sw.swarm_codec_encode if bits == 32 else sw.swarm_codec_encode_s16)(dev, codes, scales)
+    torch.cuda.synchronize()
+    codes, raw = codes.cpu().numpy().reshape(T, KV, dh), torch.int32 if bits == 32 else torch.int16
+    scales = scales.view(raw).cpu().numpy().reshape(T, KV, 2)
+    got = {n: (t if n.endswith("codes") else t.view(raw)).cpu().numpy() for n, t in cache.tensors.items()}
+    for t in range(T):
+        p, o = w.table[0, (9 + t) // page], (9 + t) % page
+        assert np.array_equal(got["k_codes"][p, :, o], codes[t]) and np.array_equal(got["v_codes"][p, :, :, o], codes[t])
+        assert np.array_equal(got["k_scales"][p, :, :, o], scales[t]) and np.array_equal(got["v_scales"][p, :, :, o], scales[t])
+
+
 def test_append_leaves_out_what_is_out_of_range():
     """Sequences whose lengths do not fit and pages that are none: nothing of them is written, everything else is."""
     import paper_2301_11913_amd as sw
@@ -241,6 +268,23 @@ def test_attention(case):
     q = w.normal(w.B * T, H, dh, std=1.5)
     words = tree_words(w.rng, w.B, T) if tree else None
     check_attention(w, q, words, run_attention(w, q, words, max_len=int((w.past + w.fresh).max()), pads=(8, 16)))
+
+
+@pytest.mark.parametrize("page", [16, 128])
+@pytest.mark.parametrize("bits", [32, 16])
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("dtype,rows", [("f32", 3), ("f32", 7), ("f32", 13), ("bf16", 3), ("bf16", 7), ("bf16", 40), ("bf16", 100)])
+def test_attention_at_every_number_of_rows(dtype, rows, dh, bits, page):
+    """Each kernel's row counts, head sizes, scales, page sizes: over several tiles and splits, with and without a tree."""
+    w = World(7000 + rows + dh + bits + page, dtype, 2, 2, dh, rows, [700, 129], page, bits, fresh=[rows, rows - 1])
+    for b in range(w.B):
+        n = int(w.fresh[b])
+        oc.append(w.pool, w.table, page, b, int(w.past[b]), w.normal(n, 2, dh), w.normal(n, 2, dh), bits)
+    q = w.normal(w.B * rows, 2, dh, std=1.5)
+    words = tree_words(w.rng, w.B, rows) if rows <= 64 else None
+    for tree in ([None, words] if rows <= 64 else [None]):
+        for max_len in (64, 1024):                                       # one workgroup for a sequence, and several
+            check_attention(w, q, tree, run_attention(w, q, tree, max_len))
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
