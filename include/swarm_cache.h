@@ -79,7 +79,7 @@ swarm_status swarm_cache_keep(const swarm_cache_config *cfg, const swarm_cache *
  * u <= t.  With a tree, tokens <= 64; tokens * n_heads / n_kv_heads <= 2^24.  A row that sees no token at all is zeros.
  * q rows (n_heads * d_head elements) are q_pitch apart, out rows out_pitch.  max_len: a bound on past + fresh that the caller knows
  * (0: what page_table can hold); it decides over how many workgroups a sequence is spread, and the workspace; a longer sequence
- * is right too, only slower.  scratch: swarm_cache_attention_workspace_bytes, 256-byte aligned, or NULL where that is 0. */
+ * is right too, only slower.  workspace: swarm_cache_attention_workspace_bytes, 256-byte aligned, or NULL where that is 0. */
 size_t swarm_cache_attention_workspace_bytes(const swarm_cache_config *cfg, int32_t tokens, int32_t max_len);
 swarm_status swarm_cache_attention(const swarm_cache_config *cfg, const swarm_cache *cache, const int32_t *page_table,
                                    const int32_t *past, const int32_t *fresh, int32_t tokens, int32_t max_len, const void *q,

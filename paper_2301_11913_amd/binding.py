@@ -382,6 +382,13 @@ def _device() -> Optional[int]:
     return _current_device() if _current_device is not None and torch.cuda.is_initialized() else None
 
 
+def _on(stream, device: Optional[int]) -> Optional[int]:
+    """_stream where the current GPU is known already."""
+    if stream is None and device is not None and _raw_stream is not None:
+        return _raw_stream(device) or None
+    return _stream(stream)
+
+
 def _refuse(t: torch.Tensor, name: str, dtypes, n: Optional[int], device: Optional[int]):
     if t.dtype not in dtypes:
         raise TypeError("%s must be %s" % (name, " or ".join(str(d) for d in dtypes)))
@@ -733,7 +740,7 @@ def swarm_cache_append(cfg: CacheConfig, cache: Cache, page_table: torch.Tensor,
     st = load_library().swarm_cache_append(cfg._ref, _pool(cfg, cache, dev), _ints(page_table, pages, "page_table", dev),
                                            _ints(past, batch, "past", dev), _ints(fresh, batch, "fresh", dev), tokens, qp, kp, vp,
                                            pitch, _ints(positions, rows, "positions", dev), 1 if rotary else 0, op, out_pitch,
-                                           _stream(stream))
+                                           _on(stream, dev))
     if st != 0:
         raise SwarmError(st, "swarm_cache_append")
 
@@ -744,7 +751,7 @@ def swarm_cache_read(cfg: CacheConfig, cache: Cache, page_table: torch.Tensor, f
     n, dev = batch * tokens * kv_width, _device()
     st = load_library().swarm_cache_read(cfg._ref, _pool(cfg, cache, dev), _ints(page_table, pages, "page_table", dev),
                                          _ints(first, batch, "first", dev), _ints(count, batch, "count", dev), tokens,
-                                         _buffer(k_out, n, dt, "k_out", dev), _buffer(v_out, n, dt, "v_out", dev), _stream(stream))
+                                         _buffer(k_out, n, dt, "k_out", dev), _buffer(v_out, n, dt, "v_out", dev), _on(stream, dev))
     if st != 0:
         raise SwarmError(st, "swarm_cache_read")
 
@@ -755,7 +762,7 @@ def swarm_cache_keep(cfg: CacheConfig, cache: Cache, page_table: torch.Tensor, p
     dev = _device()
     st = load_library().swarm_cache_keep(cfg._ref, _pool(cfg, cache, dev), _ints(page_table, pages, "page_table", dev),
                                          _ints(past, batch, "past", dev), _ints(kept, batch * tokens, "kept", dev),
-                                         _ints(n_kept, batch, "n_kept", dev), tokens, _stream(stream))
+                                         _ints(n_kept, batch, "n_kept", dev), tokens, _on(stream, dev))
     if st != 0:
         raise SwarmError(st, "swarm_cache_keep")
 
@@ -776,7 +783,7 @@ def swarm_cache_attention(cfg: CacheConfig, cache: Cache, page_table: torch.Tens
     wp, n = _workspace(workspace, dev)
     st = load_library().swarm_cache_attention(cfg._ref, _pool(cfg, cache, dev), _ints(page_table, pages, "page_table", dev),
                                               _ints(past, batch, "past", dev), _ints(fresh, batch, "fresh", dev), tokens, max_len,
-                                              qp, q_pitch, _tree(tree, rows, dev), op, out_pitch, wp, n, _stream(stream))
+                                              qp, q_pitch, _tree(tree, rows, dev), op, out_pitch, wp, n, _on(stream, dev))
     if st != 0:
         raise SwarmError(st, "swarm_cache_attention")
 
@@ -803,7 +810,7 @@ def swarm_stage_extend(cfg: StageConfig, params: List[Dict[str, torch.Tensor]], 
                                            _ints(page_table, pages, "page_table", dev), _ints(past, batch, "past", dev),
                                            _ints(fresh, batch, "fresh", dev), _ints(positions, rows, "positions", dev),
                                            _tree(tree, rows, dev), max_len, _buffer(x_in, rows * c.d_model, cfg.torch_dtype, "x_in", dev),
-                                           _buffer(x_out, rows * c.d_model, cfg.torch_dtype, "x_out", dev), wp, n, _stream(stream))
+                                           _buffer(x_out, rows * c.d_model, cfg.torch_dtype, "x_out", dev), wp, n, _on(stream, dev))
     if st != 0:
         raise SwarmError(st, "swarm_stage_extend")
 
@@ -814,7 +821,7 @@ def swarm_head_logits(cfg: HeadConfig, params: Dict[str, torch.Tensor], x: torch
     dt = torch.float32 if c.dtype == SWARM_F32 else torch.bfloat16
     wp, n = _workspace(workspace, dev)
     st = load_library().swarm_head_logits(C.byref(c), C.byref(_ptrs3(params, "w_vocab")), _buffer(x, c.tokens * c.d_model, dt, "x", dev),
-                                          _buffer(logits, c.tokens * c.vocab_rows, dt, "logits", dev), wp, n, _stream(stream))
+                                          _buffer(logits, c.tokens * c.vocab_rows, dt, "logits", dev), wp, n, _on(stream, dev))
     if st != 0:
         raise SwarmError(st, "swarm_head_logits")
 
@@ -829,6 +836,6 @@ def swarm_logits_adjust(rules: LogitsRules, logits: torch.Tensor, out: torch.Ten
     op, out_pitch = _rows(out, rows, out.shape[1], _F32, "out", dev)
     if rules_dev is not None and rules_dev != dev:
         raise ValueError("the rules are on GPU %d, the current GPU is %s" % (rules_dev, dev))
-    st = load_library().swarm_logits_adjust(rules._ref, lp, _dtype_code(logits), pitch, op, out_pitch, _stream(stream))
+    st = load_library().swarm_logits_adjust(rules._ref, lp, _dtype_code(logits), pitch, op, out_pitch, _on(stream, dev))
     if st != 0:
         raise SwarmError(st, "swarm_logits_adjust")
