@@ -1,9 +1,11 @@
 // Attention of many new tokens over the paged int8 cache, bf16: drafted trees, prompts.
 //
-// The codes are whole numbers of 8 bits, which bf16 holds exactly: a tile of 64 tokens is read once per workgroup, turned into bf16 on
-// the way into LDS (one conversion per code, one byte permutation per two) and contracted with the queries on v_mfma_f32_32x32x16_bf16.
-// The scales never touch the codes: a score is the sum over the blocks of 64 elements of (products) * (key's scale), and the weight of a
-// value is p_j times its scale, so the only roundings beyond fp32 are those of the weights to bf16.
+// The codes are whole numbers of 8 bits, which bf16 and fp16 hold exactly: a tile of 64 tokens is read once per workgroup, and on the way
+// into LDS the keys turn into bf16, as the queries are, and the values into fp16.  The products are v_mfma_f32_32x32x16.  The scales never
+// touch the codes: a score is the sum over the blocks of 64 elements of (products) * (key's scale), and the weight of a value is p_j times
+// its scale, so the only roundings beyond fp32 are those of the weights.  These are held in fp16 (a rounding of 2^-11, where bf16's 2^-8 would
+// be as large as the output's own), relative to a power of two near the values' largest scale so far: it is raised, and the sums with it
+// lowered, when a tile's scales pass it by 2^6.  A weight that is 2^-14 of that power or less has an error of 2^-25 of it instead.
 //   scores  S^T [token][query] = K Q^T, 32 tokens x 32 queries: a lane owns one query column, so a maximum or a sum needs one exchange
 //           between lanes; row 8 a + 4 b + i of the keys' operand is token 16 (a / 2) + 8 b + 4 (a % 2) + i, which leaves a lane eight
 //           consecutive tokens' weights twice:
@@ -26,12 +28,35 @@ typedef __attribute__((ext_vector_type(2))) float f32x2;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kNoExp = -100000;        // no scale yet
 // 4 prompts of 2048 tokens, 32 heads of 128: 222 us; 4 pairs at a time 225, 2 241, one 262, all 16 of an XCD 221
 constexpr int kPairs = 8;
 
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
   f32x2 v = {a, b};
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+}
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+__device__ __forceinline__ uint32_t pack2_f16(float a, float b) {
+  f32x2 v = {a, b};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2));
+}
+// four codes as fp16: 0x6400 + u is 1024 + u for a byte u, here the code + 128
+__device__ __forceinline__ uint2 codes4_f16(uint32_t w) {
+  const f16x2 back = {(_Float16)-1152.0f, (_Float16)-1152.0f};
+  w ^= 0x80808080u;
+  const f16x2 a = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, w, 0x04010400u)) + back;
+  const f16x2 b = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, w, 0x04030402u)) + back;
+  return make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b));
+}
+// the largest of a wavefront's values (not negative, as whole numbers), the same for all lanes
+template <int N>
+__device__ __forceinline__ uint32_t turned(uint32_t v) { return __builtin_amdgcn_mov_dpp(v, 0x120 + N, 0xF, 0xF, true); }
+__device__ __forceinline__ uint32_t wave_umax(uint32_t v) {
+  v = max(v, turned<8>(v)); v = max(v, turned<4>(v)); v = max(v, turned<2>(v)); v = max(v, turned<1>(v));
+  return max(max((uint32_t)__builtin_amdgcn_readlane(v, 0), (uint32_t)__builtin_amdgcn_readlane(v, 16)),
+             max((uint32_t)__builtin_amdgcn_readlane(v, 32), (uint32_t)__builtin_amdgcn_readlane(v, 48)));
 }
 // four codes as bf16: whole numbers of 8 bits, so the upper half of their fp32 form is all there is
 __device__ __forceinline__ uint2 codes4(uint32_t w) {
@@ -44,8 +69,9 @@ template <int DH> struct Stage {
   static constexpr int NB = DH / 64, CH = DH / 8;          // 16-byte chunks of a key row
   uint4 k[64 * CH];
   uint4 v[DH * 8];
-  float ks[NB][64], vs[NB][64];                            // keys' with the factor of the scores in them
+  float ks[NB][64], vs[NB][64];                            // keys' with the factor of the scores in them, values' over 2^v_exp
   uint32_t bad[NB][2];                                     // tokens whose value's scale is no finite number; 0 stands in its place
+  int v_exp[NB];
   static __device__ __forceinline__ int k_at(int key, int chunk) {
     return key * CH + (chunk ^ (DH == 128 ? key & 15 : (key >> 1) & 7));
   }
@@ -102,6 +128,9 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
   f32x16 o[DT];
   float ref = 0.f, l = 0.f;              // weights are 2^(score - ref)
   float most = -INFINITY;                // what a score may exceed ref by: nothing before the first, then 8
+  int v_exp[NB];                         // o is in units of 2^v_exp
+#pragma unroll
+  for (int blk = 0; blk < NB; ++blk) v_exp[blk] = kNoExp;
 #pragma unroll
   for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -176,7 +205,8 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
     sc = block_scale_load(wave < NB ? a.c.k_scales : a.c.v_scales, s_from, S16);              // of threads beyond SCALES: in bounds, of no use
   };
   const float factor = (DH == 64 ? 0.125f : 0.08838834764831845f) * kLog2e;
-  auto store = [&](St& st) {
+  int v_now = kNoExp;                                        // of the wavefronts that stage values' scales
+  auto store = [&](St& st, uint64_t valid) {
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
       const int idx = threadIdx.x + i * THREADS, key = idx / KP, piece = idx % KP;
@@ -187,7 +217,7 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
       const int idx = threadIdx.x + i * THREADS, d = idx >> 2, piece = idx & 3;
-      const uint2 w0 = codes4(vc[i].x), w1 = codes4(vc[i].y), w2 = codes4(vc[i].z), w3 = codes4(vc[i].w);
+      const uint2 w0 = codes4_f16(vc[i].x), w1 = codes4_f16(vc[i].y), w2 = codes4_f16(vc[i].z), w3 = codes4_f16(vc[i].w);
       st.v[St::v_at(d, 2 * piece)] = make_uint4(w0.x, w0.y, w1.x, w1.y);
       st.v[St::v_at(d, 2 * piece + 1)] = make_uint4(w2.x, w2.y, w3.x, w3.y);
     }
@@ -195,10 +225,14 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
     if (wave < NB) {
       st.ks[blk][key] = sc * factor;
     } else if (wave < 2 * NB) {
-      const bool fine = (__float_as_uint(sc) & 0x7FFFFFFFu) < 0x7F800000u;
-      const uint64_t bad = __ballot(!fine);
-      st.vs[blk][key] = fine ? sc : 0.f;
+      const bool there = (valid >> key) & 1, fine = (__float_as_uint(sc) & 0x7FFFFFFFu) < 0x7F800000u;
+      const uint64_t bad = __ballot(there && !fine);
+      const float v = there && fine ? sc : 0.f;
+      const int top = (int)(wave_umax(__float_as_uint(v) & 0x7FFFFFFFu) >> 23) - 126;      // all are below 2^top
+      if (v_now == kNoExp || top > v_now + 6) v_now = top;
+      st.vs[blk][key] = ldexpf(v, -v_now);
       if ((key & 31) == 0) st.bad[blk][key >> 5] = (uint32_t)(bad >> key);
+      if (key == 0) st.v_exp[blk] = v_now;
     }
   };
 
@@ -206,6 +240,9 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
   const int k_row = (n & 16) | ((n & 4) << 1) | ((n & 8) >> 1) | (n & 3);       // the token of this lane's row of the keys' operand
   auto half = [&](const St& st, int j0, int kh, uint64_t valid) {
     const uint32_t bad = st.bad[0][kh] | st.bad[NB - 1][kh];
+    int v_next[NB];
+#pragma unroll
+    for (int blk = 0; blk < NB; ++blk) v_next[blk] = __builtin_amdgcn_readfirstlane(st.v_exp[blk]);
     f32x16 acc[NB];
 #pragma unroll
     for (int blk = 0; blk < NB; ++blk)
@@ -269,20 +306,28 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
     if (__builtin_amdgcn_readfirstlane(bad))
       if (sees & (bad >> (8 * lh)) & 0x00FF00FFu) l = __uint_as_float(0x7FC00000u);
 #pragma unroll
+    for (int blk = 0; blk < NB; ++blk)
+      if (v_next[blk] != v_exp[blk]) {
+        const float less = ldexpf(1.0f, v_exp[blk] - v_next[blk]);           // from no scale: 0, of sums that are 0
+#pragma unroll
+        for (int d = 2 * blk; d < 2 * blk + 2; ++d) o[d] *= less;
+        v_exp[blk] = v_next[blk];
+      }
+#pragma unroll
     for (int c = 0; c < 2; ++c) {
-      bf16x8 pf[NB];
+      f16x8 pf[NB];
 #pragma unroll
       for (int blk = 0; blk < NB; ++blk) {
         const float4 s0 = *reinterpret_cast<const float4*>(&st.vs[blk][32 * kh + 16 * c + 8 * lh]);
         const float4 s1 = *reinterpret_cast<const float4*>(&st.vs[blk][32 * kh + 16 * c + 8 * lh + 4]);
         const float* w = p + 8 * c;
-        pf[blk] = __builtin_bit_cast(bf16x8, make_uint4(pack2(w[0] * s0.x, w[1] * s0.y), pack2(w[2] * s0.z, w[3] * s0.w),
-                                                        pack2(w[4] * s1.x, w[5] * s1.y), pack2(w[6] * s1.z, w[7] * s1.w)));
+        pf[blk] = __builtin_bit_cast(f16x8, make_uint4(pack2_f16(w[0] * s0.x, w[1] * s0.y), pack2_f16(w[2] * s0.z, w[3] * s0.w),
+                                                       pack2_f16(w[4] * s1.x, w[5] * s1.y), pack2_f16(w[6] * s1.z, w[7] * s1.w)));
       }
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
-        const bf16x8 vf = __builtin_bit_cast(bf16x8, st.v[St::v_at(d * 32 + n, 4 * kh + 2 * c + lh)]);
-        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[d / 2], o[d], 0, 0, 0);
+        const f16x8 vf = __builtin_bit_cast(f16x8, st.v[St::v_at(d * 32 + n, 4 * kh + 2 * c + lh)]);
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pf[d / 2], o[d], 0, 0, 0);
       }
     }
   };
@@ -291,7 +336,7 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
     Pages pg = pages_of(first);
     uint64_t valid = valid_of(first, pg);
     load(first, pg);
-    store(stage[0]);
+    store(stage[0], valid);
     if (first + 1 < end) pg = pages_of(first + 1);
     __syncthreads();
     for (int tile = first; tile < end; ++tile) {
@@ -310,12 +355,16 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
       } else {
         if (j0 + 32 * key_wave < outer) half(st, j0, key_wave, valid);
       }
-      if (more) store(stage[(tile + 1 - first) & 1]);
+      if (more) store(stage[(tile + 1 - first) & 1], valid_next);
       valid = valid_next;
       __syncthreads();
     }
   }
 
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[d][e] = ldexpf(o[d][e], v_exp[d / 2]);
   l += __shfl_xor(l, 32, 64);
   float m = most == -INFINITY ? -INFINITY : ref;
   if constexpr (KW == 2) {                                   // the second half's results through LDS: [row wavefront][register][lane]

@@ -340,6 +340,28 @@ def test_attention_of_queries_of_any_size(dtype, T):
     check_attention(w, q, None, run_attention(w, q, None))
 
 
+@pytest.mark.parametrize("dtype,T", [("f32", 1), ("f32", 9), ("bf16", 1), ("bf16", 7), ("bf16", 40), ("bf16", 100)])
+@pytest.mark.parametrize("how", ["rising", "falling", "mixed", "tiny", "large", "zero first"])
+def test_attention_of_values_of_any_size(dtype, T, how):
+    """Values whose scales differ by many powers of two from token to token and tile to tile."""
+    w = World(4700 + T, dtype, 2, 2, 128, T, [0], 32, 32)
+    n = 400
+    w.past[0] = n
+    w.table_pages = -(-(n + T) // 32)
+    w.table = w.rng.permutation(w.table_pages + 2)[:w.table_pages].reshape(1, -1).astype(np.int32)
+    for name, a in list(w.pool.items()):
+        w.pool[name] = np.zeros((w.table_pages + 2,) + a.shape[1:], a.dtype)
+    size = {"rising": np.linspace(-40, 10, n + T), "falling": np.linspace(10, -40, n + T), "mixed": w.rng.uniform(-12, 12, n + T),
+            "tiny": np.full(n + T, -100.0), "large": np.full(n + T, 90.0), "zero first": np.zeros(n + T)}[how]
+    v = w.normal(n + T, 2, 128) * 2.0 ** size[:, None, None]
+    if how == "zero first":
+        v[:200] = 0.0
+    oc.append(w.pool, w.table, 32, 0, 0, w.normal(n + T, 2, 128), v, 32)
+    q = w.normal(T, 2, 128)
+    for max_len in (64, 1024):
+        check_attention(w, q, None, run_attention(w, q, None, max_len))
+
+
 @pytest.mark.parametrize("dtype,T", [("f32", 1), ("bf16", 1), ("bf16", 80)])
 def test_what_is_no_number_reaches_the_rows_that_see_it(dtype, T):
     w = World(4500 + T, dtype, 2, 2, 64, T, [100, 30], 16, 32)
