@@ -405,7 +405,7 @@ Cut cut_of(const swarm_cache_config* c, int tokens, int max_len) {
   Cut k{};
   const int rows = tokens * (c->n_heads / c->n_kv_heads);
   // bf16, 8 sequences of 4000 tokens, 32 heads, with 4 / 5 / 8 / 16 / 32 rows each: the kernel of bytes 56 / 74 / 75 / 96 / 149 us at
-  // d_head 128 and 32 / - / 34 / 62 / 96 at 64, the kernel of many rows 65 / 65 / 64 / 67 / 69 and 42 / - / 42 / 42 / 43
+  // d_head 128 and 32 / - / 34 / 62 / 96 at 64, the kernel of many rows 66 / 69 / 69 / 75 / 75 and - / - / 42 / 41 / 43
   k.many = c->dtype == SWARM_BF16 && rows > (c->d_head == 64 ? 8 : 4);
   if (k.many) {
     k.row_tiles = rows <= 64 ? 2 : 4;
@@ -421,7 +421,7 @@ Cut cut_of(const swarm_cache_config* c, int tokens, int max_len) {
   const long long tiles = (len + kTile - 1) / kTile, whole = (long long)c->batch * c->n_kv_heads * k.row_groups;
   // As many workgroups as are resident, each of four tiles at least (one for every wavefront): 512, with many rows of d_head 64 768.
   // 32 sequences of up to 8192 tokens / one of 131072 with 8 heads: 213 / 57 us; with 1024 213 / 60, 2048 246 / 70, 4096 271 / 86.
-  // Trees of 33 over 2011 tokens, d_head 128: 43 us; with 256 50, 768 47, 1024 49.  32 rows over 8 x 4000 tokens at d_head 64: 43 us; with 512
+  // Trees of 33 over 2011 tokens, d_head 128 (weights in bf16): 43 us; with 256 50, 768 47, 1024 49.  32 rows over 8 x 4000 tokens at d_head 64: 43 us; with 512
   // 49, 1024 53.
   const long long target = k.many && c->d_head == 64 ? 768 : 512;
   const long long chunk = std::max(4ll, std::min<long long>(1ll << 24, (whole * tiles + target - 1) / target));

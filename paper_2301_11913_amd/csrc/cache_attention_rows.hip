@@ -29,7 +29,7 @@ typedef __attribute__((ext_vector_type(16))) float f32x16;
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kNoExp = -100000;        // no scale yet
-// 4 prompts of 2048 tokens, 32 heads of 128: 222 us; 4 pairs at a time 225, 2 241, one 262, all 16 of an XCD 221
+// 4 prompts of 2048 tokens, 32 heads of 128 (weights in bf16): 222 us; 4 pairs at a time 225, 2 241, one 262, all 16 of an XCD 221
 constexpr int kPairs = 8;
 
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
@@ -70,8 +70,8 @@ template <int DH> struct Stage {
   uint4 k[64 * CH];
   uint4 v[DH * 8];
   float ks[NB][64], vs[NB][64];                            // keys' with the factor of the scores in them, values' over 2^v_exp
-  uint32_t bad[NB][2];                                     // tokens whose value's scale is no finite number; 0 stands in its place
-  int v_exp[NB];
+  // v_exp, and (as bits of two words) the tokens whose value's scale is no finite number; 0 stands in its place
+  uint4 about[NB];
   static __device__ __forceinline__ int k_at(int key, int chunk) {
     return key * CH + (chunk ^ (DH == 128 ? key & 15 : (key >> 1) & 7));
   }
@@ -231,18 +231,16 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
       const int top = (int)(wave_umax(__float_as_uint(v) & 0x7FFFFFFFu) >> 23) - 126;      // all are below 2^top
       if (v_now == kNoExp || top > v_now + 6) v_now = top;
       st.vs[blk][key] = ldexpf(v, -v_now);
-      if ((key & 31) == 0) st.bad[blk][key >> 5] = (uint32_t)(bad >> key);
-      if (key == 0) st.v_exp[blk] = v_now;
+      if (key == 0) st.about[blk] = make_uint4((uint32_t)v_now, (uint32_t)bad, (uint32_t)(bad >> 32), 0);
     }
   };
 
   // 32 tokens of a tile: scores, weights, output
   const int k_row = (n & 16) | ((n & 4) << 1) | ((n & 8) >> 1) | (n & 3);       // the token of this lane's row of the keys' operand
   auto half = [&](const St& st, int j0, int kh, uint64_t valid) {
-    const uint32_t bad = st.bad[0][kh] | st.bad[NB - 1][kh];
-    int v_next[NB];
+    uint4 about[NB];                                         // asked for here, looked at behind the softmax
 #pragma unroll
-    for (int blk = 0; blk < NB; ++blk) v_next[blk] = __builtin_amdgcn_readfirstlane(st.v_exp[blk]);
+    for (int blk = 0; blk < NB; ++blk) about[blk] = st.about[blk];
     f32x16 acc[NB];
 #pragma unroll
     for (int blk = 0; blk < NB; ++blk)
@@ -303,16 +301,20 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
       l += p[e];
     }
     // a value that is infinite or none goes to all of the rows that see it, and to no others
+    const uint32_t bad = kh == 0 ? about[0].y | about[NB - 1].y : about[0].z | about[NB - 1].z;
     if (__builtin_amdgcn_readfirstlane(bad))
       if (sees & (bad >> (8 * lh)) & 0x00FF00FFu) l = __uint_as_float(0x7FC00000u);
 #pragma unroll
-    for (int blk = 0; blk < NB; ++blk)
-      if (v_next[blk] != v_exp[blk]) {
-        const float less = ldexpf(1.0f, v_exp[blk] - v_next[blk]);           // from no scale: 0, of sums that are 0
+    for (int blk = 0; blk < NB; ++blk) {
+      if (KW == 1 && kh == 1) break;                         // the tile's first half has seen to it
+      const int next = __builtin_amdgcn_readfirstlane((int)about[blk].x);
+      if (next != v_exp[blk]) {
+        const float less = ldexpf(1.0f, v_exp[blk] - next);  // from no scale: 0, of sums that are 0
 #pragma unroll
         for (int d = 2 * blk; d < 2 * blk + 2; ++d) o[d] *= less;
-        v_exp[blk] = v_next[blk];
+        v_exp[blk] = next;
       }
+    }
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
       f16x8 pf[NB];

@@ -84,9 +84,10 @@ def attention_bound(dtype, out, mean_abs, size, n, v_max):
       its score is a sum of d_head / 64 products of whole numbers and two scales, about 16 roundings of 2^-24 of at most
       `size` each, which the exponential turns into a relative error; the exponent and the maximum it is taken from have the
       same size (8 more), exp itself and the running sums add one rounding per 64 tokens and 64 for the rest;
-      bf16: the weight itself may be rounded to bf16 (2^-8).
+      bf16: the weight itself may be rounded to fp16 (2^-11).
     Numerator and denominator each carry it: 2 eps of the weighted mean of |v|.  Weights may also be held as whole numbers of
-    2^-22 of the largest one (bf16) or 2^-30 (fp32): n of them against a sum of at least 1.  At the end half a step of the type."""
-    eps = 2.0 ** -24 * (24 * size[..., None] + n / 64 + 64) + (2.0 ** -8 if dtype == "bf16" else 0.0)
+    2^-22 of the largest one (bf16; below fp16's normal range 2^-24) or 2^-30 (fp32): n of them against a sum of at least 1.  At the end half a
+    step of the type."""
+    eps = 2.0 ** -24 * (24 * size[..., None] + n / 64 + 64) + (2.0 ** -11 if dtype == "bf16" else 0.0)
     whole = n * v_max * (2.0 ** -22 if dtype == "bf16" else 2.0 ** -30)
     return 2 * eps * mean_abs + whole + HALF_STEP[dtype] * np.abs(out) + 1e-30
