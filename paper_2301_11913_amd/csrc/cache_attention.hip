@@ -80,7 +80,9 @@ __global__ __launch_bounds__(kThreads) void cache_attention_bytes_kernel(AttnArg
   __shared__ __attribute__((aligned(16))) char lds[kQBytes + kPBytes > kOBytes ? kQBytes + kPBytes : kOBytes];
   __shared__ float q_scale[Q][NB];
   const int lane = threadIdx.x & 63, n = lane & 15, lg = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);      // the same for all lanes: loops and branches on it are scalar
+  // The same for all lanes, so that the loop over tiles is scalar.  (As a loop masked by lanes it was compiled wrongly:
+  // the values' scales were overwritten before their use.)
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int unit = blockIdx.x;
   const int split = unit % a.splits; unit /= a.splits;
   const int g = unit % a.c.KV; unit /= a.c.KV;
@@ -250,7 +252,7 @@ __global__ __launch_bounds__(kThreads) void cache_attention_bytes_kernel(AttnArg
         }
         top = largest();
       }
-      const int ex = (int)(top >> 23) - 126;
+      const int ex = max((int)(top >> 23) - 126, -110);        // the way back, 2^(ex - BITS), is a number
 #pragma unroll
       for (int c = 0; c < 4; ++c) vn[blk][c] = ldexpf(vn[blk][c], BITS - ex);
       back[blk] = ldexpf(1.0f, ex - BITS);
