@@ -4,8 +4,11 @@
 // into LDS the keys turn into bf16, as the queries are, and the values into fp16.  The products are v_mfma_f32_32x32x16.  The scales never
 // touch the codes: a score is the sum over the blocks of 64 elements of (products) * (key's scale), and the weight of a value is p_j times
 // its scale, so the only roundings beyond fp32 are those of the weights.  These are held in fp16 (a rounding of 2^-11, where bf16's 2^-8 would
-// be as large as the output's own), relative to a power of two near the values' largest scale so far: it is raised, and the sums with it
-// lowered, when a tile's scales pass it by 2^6.  A weight that is 2^-14 of that power or less has an error of 2^-25 of it instead.
+// be as large as the output's own) relative to a power of two, which is the unit of the query's sums as well.  The unit puts the scales
+// between 2 and 2^7, so a weight has an error of half an fp16 step or of 2^-26 of what it would be with p_j = 1, whichever is more.  It
+// follows the tiles up and down, up no further than a query's own weights ask for.  A tile whose scales other than 0 lie further apart than
+// 2^6 is gone through once for each range of 2^6 that it has tokens in.  So a value that a row does not see, or sees with next to no weight,
+// costs the others none of their digits.
 //   scores  S^T [token][query] = K Q^T, 32 tokens x 32 queries: a lane owns one query column, so a maximum or a sum needs one exchange
 //           between lanes; row 8 a + 4 b + i of the keys' operand is token 16 (a / 2) + 8 b + 4 (a % 2) + i, which leaves a lane eight
 //           consecutive tokens' weights twice:
@@ -29,7 +32,11 @@ typedef __attribute__((ext_vector_type(2))) float f32x2;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kNoExp = -100000;        // no scale yet
+constexpr int kNoExp = -100000;        // no unit yet
+constexpr int kRange = 6;              // exponents of the scales that go together
+// How far below its largest weight the unit of a query's sums may be.  A weight is below 2^15 units (2^8 by the running maximum, 2^7 by the
+// scale), a code is below 2^7 and there are up to 2^30 tokens, so sums are numbers down to a unit of 2^-72 of that weight's.
+constexpr int kFall = 72;
 // 4 prompts of 2048 tokens, 32 heads of 128 (weights in bf16): 222 us; 4 pairs at a time 225, 2 241, one 262, all 16 of an XCD 221
 constexpr int kPairs = 8;
 
@@ -59,6 +66,7 @@ __device__ __forceinline__ uint32_t wave_umax(uint32_t v) {
   return max(max((uint32_t)__builtin_amdgcn_readlane(v, 0), (uint32_t)__builtin_amdgcn_readlane(v, 16)),
              max((uint32_t)__builtin_amdgcn_readlane(v, 32), (uint32_t)__builtin_amdgcn_readlane(v, 48)));
 }
+__device__ __forceinline__ uint32_t wave_umin(uint32_t v) { return ~wave_umax(~v); }
 // four codes as bf16: whole numbers of 8 bits, so the upper half of their fp32 form is all there is
 __device__ __forceinline__ uint2 codes4(uint32_t w) {
   const uint32_t a = __float_as_uint((float)(int8_t)w), b = __float_as_uint((float)(int8_t)(w >> 8));
@@ -70,9 +78,12 @@ template <int DH> struct Stage {
   static constexpr int NB = DH / 64, CH = DH / 8;          // 16-byte chunks of a key row
   uint4 k[64 * CH];
   uint4 v[DH * 8];
-  float ks[NB][64], vs[NB][64];                            // keys' with the factor of the scores in them, values' over 2^v_exp
-  // v_exp, and (as bits of two words) the tokens whose value's scale is no finite number; 0 stands in its place
+  float ks[NB][64], vs[NB][64];                            // keys' with the factor of the scores in them, values' over 2^unit
+  float none[64];                                          // zeros
+  // .x: the unit times 4, and 2 where the scales lie apart: unit[] holds one for each token then, and 1 where .y, .z are not 0: the tokens, by
+  // bits, whose value's scale is no finite number (0 stands in its place)
   uint4 about[NB];
+  int unit[NB][64];
   static __device__ __forceinline__ int k_at(int key, int chunk) {
     return key * CH + (chunk ^ (DH == 128 ? key & 15 : (key >> 1) & 7));
   }
@@ -129,9 +140,9 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
   f32x16 o[DT];
   float ref = 0.f, l = 0.f;              // weights are 2^(score - ref)
   float most = -INFINITY;                // what a score may exceed ref by: nothing before the first, then 8
-  int v_exp[NB];                         // o is in units of 2^v_exp
+  int v_exp[NB], v_top[NB];              // the query's o is in units of 2^v_exp; its largest weight was about 2^v_top
 #pragma unroll
-  for (int blk = 0; blk < NB; ++blk) v_exp[blk] = kNoExp;
+  for (int blk = 0; blk < NB; ++blk) v_exp[blk] = v_top[blk] = kNoExp;
 #pragma unroll
   for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -229,19 +240,25 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
       const bool there = (valid >> key) & 1, fine = (__float_as_uint(sc) & 0x7FFFFFFFu) < 0x7F800000u;
       const uint64_t bad = __ballot(there && !fine);
       const float v = there && fine ? sc : 0.f;
-      const int top = (int)(wave_umax(__float_as_uint(v) & 0x7FFFFFFFu) >> 23) - 126;      // all are below 2^top
-      if (v_now == kNoExp || top > v_now + 6) v_now = top;
-      st.vs[blk][key] = ldexpf(v, -v_now);
-      if (key == 0) st.about[blk] = make_uint4((uint32_t)v_now, (uint32_t)bad, (uint32_t)(bad >> 32), 0);
+      const uint32_t bits = __float_as_uint(v) & 0x7FFFFFFFu;
+      const int ex = (int)(bits >> 23);                      // v is from 2^(ex - 127) to below 2^(ex - 126)
+      bool apart = false;
+      if (__ballot(bits != 0 && (uint32_t)(ex - 128 - v_now) >= (uint32_t)kRange)) {
+        const int hi = (int)(wave_umax(bits) >> 23), lo = (int)((wave_umin(bits - 1) + 1) >> 23);    // of those that are not 0
+        apart = lo == 0 || hi - lo >= kRange;
+        if (!apart) v_now = lo - 128 - (kRange - 1 - (hi - lo)) / 2;
+      }
+      const int unit = apart && bits != 0 ? ex - ex % kRange - 128 : v_now;
+      st.vs[blk][key] = ldexpf(v, -unit);
+      if (apart) st.unit[blk][key] = unit;
+      if (key == 0) st.about[blk] = make_uint4((uint32_t)(v_now * 4 + (apart ? 2 : 0) + (bad ? 1 : 0)), (uint32_t)bad, (uint32_t)(bad >> 32), 0);
     }
   };
 
   // 32 tokens of a tile: scores, weights, output
   const int k_row = (n & 16) | ((n & 4) << 1) | ((n & 8) >> 1) | (n & 3);       // the token of this lane's row of the keys' operand
-  auto half = [&](const St& st, int j0, int kh, uint64_t valid) {
-    uint4 about[NB];                                         // asked for here, looked at behind the softmax
-#pragma unroll
-    for (int blk = 0; blk < NB; ++blk) about[blk] = st.about[blk];
+  // odd: not all queries' sums are in the tile's unit(s), or there is a bad value: for the block `which` alone then
+  auto half = [&](const St& st, int j0, int kh, uint64_t valid, const int (&unit)[NB], bool odd, int which, bool bad_ones) {
     f32x16 acc[NB];
 #pragma unroll
     for (int blk = 0; blk < NB; ++blk)
@@ -287,6 +304,8 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
         const bool fresh = most == -INFINITY;
         const float next = fresh ? top : ref + fmaxf(top, 0.f), up = next - ref;
         const float keep = fresh ? 1.f : __builtin_amdgcn_exp2f(-up);        // fresh: there is nothing yet
+#pragma unroll
+        for (int blk = 0; blk < NB; ++blk) v_top[blk] -= fresh ? 0 : (int)fminf(up, 1000.f);
         ref = next;
         most = 8.0f;
         l *= keep;
@@ -296,33 +315,54 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
         for (int e = 0; e < 16; ++e) p[e] -= up;
       }
     }
+    const float* vs[NB];
+#pragma unroll
+    for (int blk = 0; blk < NB; ++blk) vs[blk] = odd && blk != which ? st.none : st.vs[blk];
+    float counted = 1.0f;                                    // what makes a weight one of the sum l
+    if (odd) {
+      // a value that is infinite or none goes to all of the rows that see it, and to no others
+      if (bad_ones) {
+        const uint32_t bad = kh == 0 ? st.about[0].y | st.about[NB - 1].y : st.about[0].z | st.about[NB - 1].z;
+        if (sees & (bad >> (8 * lh)) & 0x00FF00FFu) l = __uint_as_float(0x7FC00000u);
+      }
+      // The sums to the unit, or to that of the query's largest weight here where that is less but more than the sums' own (a query
+      // without weights here adds zeros in any unit); the weights to what they are in that unit.  What is too far below the sums is left out.
+      float top = p[0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) top = fmaxf(top, p[e]);
+      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      const bool any = top > -126.0f;
+      const int up = (int)ceilf(any ? top : 0.f);            // the weights are 2^up at most
+      int by = 0;
+#pragma unroll
+      for (int blk = 0; blk < NB; ++blk) {
+        if (blk != which) continue;
+        const int next = unit[blk], have = v_exp[blk];
+        const bool first = v_top[blk] == kNoExp, counts = next >= have || next >= v_top[blk] - kFall;
+        const int at = !real || (first && !any) ? next : !any || !counts ? have : next < have ? next : min(next, max(next + up, have));
+        const float less = ldexpf(1.0f, have - at);          // from no unit: 0, of sums that are 0
+#pragma unroll
+        for (int d = 2 * blk; d < 2 * blk + 2; ++d) o[d] *= less;
+        by = !any ? 0 : counts ? next - at : -60;            // 2^-60: nothing in fp16
+        v_exp[blk] = at;
+        v_top[blk] = any && counts ? max(v_top[blk], next + up) : v_top[blk];
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) p[e] += (float)by;
+      counted = which == 0 ? ldexpf(1.0f, -by) : 0.f;
+    }
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
       p[e] = __builtin_amdgcn_exp2f(p[e]);
-      l += p[e];
-    }
-    // a value that is infinite or none goes to all of the rows that see it, and to no others
-    const uint32_t bad = kh == 0 ? about[0].y | about[NB - 1].y : about[0].z | about[NB - 1].z;
-    if (__builtin_amdgcn_readfirstlane(bad))
-      if (sees & (bad >> (8 * lh)) & 0x00FF00FFu) l = __uint_as_float(0x7FC00000u);
-#pragma unroll
-    for (int blk = 0; blk < NB; ++blk) {
-      if (KW == 1 && kh == 1) break;                         // the tile's first half has seen to it
-      const int next = __builtin_amdgcn_readfirstlane((int)about[blk].x);
-      if (next != v_exp[blk]) {
-        const float less = ldexpf(1.0f, v_exp[blk] - next);  // from no scale: 0, of sums that are 0
-#pragma unroll
-        for (int d = 2 * blk; d < 2 * blk + 2; ++d) o[d] *= less;
-        v_exp[blk] = next;
-      }
+      l = fmaf(p[e], counted, l);
     }
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
       f16x8 pf[NB];
 #pragma unroll
       for (int blk = 0; blk < NB; ++blk) {
-        const float4 s0 = *reinterpret_cast<const float4*>(&st.vs[blk][32 * kh + 16 * c + 8 * lh]);
-        const float4 s1 = *reinterpret_cast<const float4*>(&st.vs[blk][32 * kh + 16 * c + 8 * lh + 4]);
+        const float4 s0 = *reinterpret_cast<const float4*>(vs[blk] + 32 * kh + 16 * c + 8 * lh);
+        const float4 s1 = *reinterpret_cast<const float4*>(vs[blk] + 32 * kh + 16 * c + 8 * lh + 4);
         const float* w = p + 8 * c;
         pf[blk] = __builtin_bit_cast(f16x8, make_uint4(pack2_f16(w[0] * s0.x, w[1] * s0.y), pack2_f16(w[2] * s0.z, w[3] * s0.w),
                                                        pack2_f16(w[4] * s1.x, w[5] * s1.y), pack2_f16(w[6] * s1.z, w[7] * s1.w)));
@@ -335,6 +375,7 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
     }
   };
 
+  if (threadIdx.x < 128) stage[threadIdx.x >> 6].none[threadIdx.x & 63] = 0.f;
   if (first < end) {
     Pages pg = pages_of(first);
     uint64_t valid = valid_of(first, pg);
@@ -344,6 +385,10 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
     __syncthreads();
     for (int tile = first; tile < end; ++tile) {
       const bool more = tile + 1 < end;
+      const St& st = stage[(tile - first) & 1];
+      int head[NB];                                          // asked for here, looked at behind the next tile's loads
+#pragma unroll
+      for (int blk = 0; blk < NB; ++blk) head[blk] = (int)st.about[blk].x;
       uint64_t valid_next = 0;
       if (more) {
         load(tile + 1, pg);
@@ -351,12 +396,48 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
         if (tile + 2 < end) pg = pages_of(tile + 2);
       }
       const int j0 = tile * kAttnTile;
-      const St& st = stage[(tile - first) & 1];
-      if constexpr (KW == 1) {
-        if (j0 < outer) half(st, j0, 0, valid);
-        if (j0 + 32 < outer) half(st, j0, 1, valid);
-      } else {
-        if (j0 + 32 * key_wave < outer) half(st, j0, key_wave, valid);
+      int unit[NB], flags = 0;
+      bool moves = false;
+#pragma unroll
+      for (int blk = 0; blk < NB; ++blk) {
+        head[blk] = __builtin_amdgcn_readfirstlane(head[blk]);
+        flags |= head[blk] & 3;
+        unit[blk] = head[blk] >> 2;
+        if (tile == first && !(head[blk] & 2)) v_exp[blk] = unit[blk];          // of sums that are 0 yet
+        moves |= v_exp[blk] != unit[blk];
+      }
+      const bool odd = flags != 0 || __ballot(moves) != 0;
+      if (__builtin_expect(!odd, 1)) {
+        if constexpr (KW == 1) {
+          if (j0 < outer) half(st, j0, 0, valid, unit, false, 0, false);
+          if (j0 + 32 < outer) half(st, j0, 1, valid, unit, false, 0, false);
+        } else {
+          if (j0 + 32 * key_wave < outer) half(st, j0, key_wave, valid, unit, false, 0, false);
+        }
+      }
+      // for both blocks in turn, for every pair of units there is; the tokens that are left are the same for all lanes, as the loop has to know
+      uint64_t rest = !odd ? 0 : (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(valid >> 32)) << 32 |
+                                 (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)valid);
+#pragma nounroll
+      while (__builtin_expect(rest != 0, 0)) {
+#pragma unroll
+        for (int blk = 0; blk < NB; ++blk) v_top[blk] = most == -INFINITY ? v_top[blk] : max(v_top[blk], v_exp[blk]);
+        uint64_t now = rest;
+        if (flags & 2) {
+          const int of = __builtin_ctzll(rest);
+#pragma unroll
+          for (int blk = 0; blk < NB; ++blk) {
+            const int mine = head[blk] & 2 ? st.unit[blk][lane] : unit[blk];
+            unit[blk] = __builtin_amdgcn_readlane(mine, of);
+            now &= __ballot(mine == unit[blk]);
+          }
+        }
+        rest &= ~now;
+#pragma nounroll
+        for (int i = 0; i < NB * (KW == 1 ? 2 : 1); ++i) {
+          const int kh = KW == 1 ? i & 1 : key_wave;
+          if (j0 + 32 * kh < outer) half(st, j0, kh, now, unit, true, KW == 1 ? i >> 1 : i, flags & 1);
+        }
       }
       if (more) store(stage[(tile + 1 - first) & 1], valid_next);
       valid = valid_next;

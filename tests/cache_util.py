@@ -91,3 +91,69 @@ def attention_bound(dtype, out, mean_abs, size, n, v_max):
     eps = 2.0 ** -24 * (24 * size[..., None] + n / 64 + 64) + (2.0 ** -11 if dtype == "bf16" else 0.0)
     whole = n * v_max * (2.0 ** -22 if dtype == "bf16" else 2.0 ** -30)
     return 2 * eps * mean_abs + whole + HALF_STEP[dtype] * np.abs(out) + 1e-30
+
+
+class RowBound:
+    """Attention of one sequence's rows and how far each element of it may be off, by what that row sees and nothing else.  With
+    p_j = exp(score_j - largest score) and L = sum p_j >= 1, of the tokens that a row sees:
+      2 eps sum p_j |v_j| / L    a score is a sum of d_head / 64 products and two scales, about 16 roundings of 2^-24 of at most `size` each,
+                                 which the exponential turns into a relative error; the maximum it is taken from adds 8; exp and the
+                                 running sums one rounding per 64 tokens and 64 for the rest.  Numerator and denominator carry it
+      2^-11 p_j |v_j|            bf16: a weight is rounded to 11 bits, half a step off at most, up or down by chance: the sum of n such errors
+                                 is below 7 times the root of the sum of their squares but for 2 exp(-49 / 2) of all cases
+      2^-26 |v_j|                or, where that is more, it is held to 2^-26 of what the value would have with the weight 1; to 2^-24 of the
+                                 largest of all weights times scales where that is less
+      2^-56 of that largest      a weight times its scale may be left out below (include/swarm_cache.h), times a code
+    each over L, then half a step of the type, and its smallest numbers."""
+
+    def __init__(self, dtype, q, k, v, see):
+        n, H, dh = q.shape
+        group = H // k.shape[1]
+        self.out, self.bound = np.zeros((n, H, dh)), np.zeros((n, H, dh))
+        for h in range(H):
+            g = h // group
+            s = np.where(see, q[:, h] @ k[:, g].T / np.sqrt(dh), -np.inf)
+            top = s.max(axis=1, keepdims=True, initial=-np.inf)
+            p = np.where(see, np.exp(s - np.where(np.isfinite(top), top, 0.0)), 0.0)
+            total = p.sum(axis=1, keepdims=True)
+            total = np.where(total == 0, 1.0, total)
+            size = np.where(see, np.abs(q[:, h]) @ np.abs(k[:, g]).T / np.sqrt(dh), 0.0).max(axis=1, initial=0.0)[:, None]
+            a = np.abs(v[:, g])
+            eps = 2.0 ** -24 * (24 * size + see.shape[1] / 64 + 64)
+            off = 2 * eps * (p @ a)
+            if dtype == "bf16":
+                off += 2.0 ** -11 * np.minimum(p @ a, 7 * np.sqrt((p * p) @ (a * a)))
+            for i in range(0, dh, 64):
+                scale = a[:, i:i + 64].max(axis=1, keepdims=True) / 127
+                most = np.where(see, p * scale.T, 0.0).max(axis=1, keepdims=True, initial=0.0)
+                part = np.minimum(1.0, 4.0 * most / np.where(scale == 0, 1.0, scale).T)              # [rows, tokens]
+                off[:, i:i + 64] += 2.0 ** -26 * np.where(see, part, 0.0) @ a[:, i:i + 64] + 127 * 2.0 ** -56 * most * see.sum(1, keepdims=True)
+            off /= total
+            self.out[:, h] = (p @ v[:, g]) / total
+            self.bound[:, h] = 1.01 * off + HALF_STEP[dtype] * np.abs(self.out[:, h]) + (2.0 ** -133 if dtype == "bf16" else 2.0 ** -140)
+
+
+def seen_by_rows(w, words, b):
+    """keys, values and which tokens each new row of sequence b sees; zeros in place of what none of them does."""
+    n, new = int(w.past[b]), int(w.fresh[b])
+    k, v, there = oc.read(w.pool, w.table, w.page, b, list(range(n + new)))
+    see = np.ones((new, n + new), dtype=bool)
+    for t in range(new):
+        for u in range(new):
+            see[t, n + u] = u <= t if words is None else bool(int(words[b, t]) >> u & 1)
+    see &= there[None]
+    unseen = ~see.any(axis=0)
+    k[unseen], v[unseen] = 0.0, 0.0
+    return k, v, see
+
+
+def check_rows(w, q, words, got):
+    """got [B, T, H, d_head] against the oracle, every row within its own bound."""
+    for b in range(w.B):
+        new = int(w.fresh[b])
+        if new == 0:
+            continue
+        want = RowBound(w.dtype, q.reshape(w.B, w.T, w.H, w.dh)[b, :new], *seen_by_rows(w, words, b))
+        assert np.all(np.isfinite(got[b, :new]))
+        off = np.abs(got[b, :new] - want.out) / want.bound
+        assert np.all(off <= 1), (b, float(off.max()), np.unravel_index(off.argmax(), off.shape))

@@ -1,0 +1,75 @@
+"""Attention over the cache where values differ by many powers of two: every row within a bound of what that row sees."""
+import numpy as np
+import pytest
+
+from cache_util import World, check_rows, tree_words
+from oracle import cache as oc
+from test_gpu_cache import ATTENTION, run_attention
+
+pytestmark = pytest.mark.gpu
+
+ROWS = [("f32", 64, 3), ("f32", 64, 13), ("f32", 128, 9), ("f32", 128, 40), ("bf16", 64, 3), ("bf16", 64, 7), ("bf16", 128, 3),
+        ("bf16", 64, 20), ("bf16", 64, 100), ("bf16", 128, 20), ("bf16", 128, 64), ("bf16", 128, 100)]
+MANY = [(dtype, dh, T) for dtype, dh, T in ROWS if dtype == "bf16" and T > 8]
+
+
+def world(seed, dtype, dh, T, past, bits=32):
+    """Two heads; the new tokens' keys and values are there to be changed before they are appended."""
+    w = World(seed, dtype, 2, 2, dh, T, [past], 32, bits)
+    return w, w.normal(T, 2, dh), w.normal(T, 2, dh), w.normal(T, 2, dh)
+
+
+def both_cuts(w, q, words):
+    for max_len in (64, 1024):                                           # one workgroup for a sequence, and several
+        check_rows(w, q, words, run_attention(w, q, words, max_len))
+
+
+@pytest.mark.parametrize("power", [14, 22, 30, 100])
+@pytest.mark.parametrize("past", [0, 200])
+@pytest.mark.parametrize("dtype,dh,T", MANY)
+def test_what_a_row_does_not_see_costs_it_nothing(dtype, dh, T, past, power):
+    """A later token of a prompt, or another branch of a tree, with values of another size."""
+    w, q, k, v = world(8000 + T + power, dtype, dh, T, past)
+    v[T // 2] *= 2.0 ** power
+    oc.append(w.pool, w.table, 32, 0, past, k, v, 32)
+    both_cuts(w, q, None)
+    if T <= 64:
+        words = tree_words(w.rng, 1, T)
+        words[0] &= ~np.uint64(1 << (T // 2))                            # of the branch, its own token alone sees it
+        words[0, T // 2] |= np.uint64(1 << (T // 2))
+        both_cuts(w, q, words)
+
+
+@pytest.mark.parametrize("power", [24, 60])
+@pytest.mark.parametrize("at", [3, 90, 240])
+@pytest.mark.parametrize("dtype,dh,T", MANY)
+def test_what_a_row_sees_with_next_to_no_weight_costs_it_nothing(dtype, dh, T, at, power):
+    """One token's values are 2^24 (2^60) times the others', its weight e^-60 (e^-85) of theirs."""
+    n = 256
+    w = World(8200 + T + at, dtype, 2, 2, dh, T, [n], 32, 32)
+    k, v = w.normal(n + T, 2, dh), w.normal(n + T, 2, dh)
+    q = w.normal(T, 2, dh)
+    q[..., 0] = 8.0
+    k[..., 0] = 0.0
+    k[at, :, 0] = -(60.0 if power == 24 else 85.0) * np.sqrt(dh) / 8
+    v[at] *= 2.0 ** power
+    oc.append(w.pool, w.table, 32, 0, 0, k, v, 32)
+    both_cuts(w, q, None)
+
+
+@pytest.mark.parametrize("dtype,dh,T", MANY)
+@pytest.mark.parametrize("how", ["rising", "falling", "mixed", "far apart", "one element", "tiny", "zero first"])
+def test_values_of_any_size(dtype, dh, T, how):
+    """Scales that change from token to token and tile to tile.  `one element`: a value is large in one place and its other codes are 0,
+    so that the rest of the row's elements are the other tokens' alone."""
+    n = 400
+    w = World(8400 + T, dtype, 2, 2, dh, T, [n], 32, 32)
+    size = {"rising": np.linspace(-40, 10, n + T), "falling": np.linspace(10, -40, n + T), "mixed": w.rng.uniform(-12, 12, n + T),
+            "far apart": w.rng.choice([-100.0, -50.0, 0.0, 50.0, 90.0], n + T), "tiny": np.full(n + T, -100.0)}.get(how, np.zeros(n + T))
+    k, v = w.normal(n + T, 2, dh), w.normal(n + T, 2, dh) * 2.0 ** size[:, None, None]
+    if how == "one element":
+        v[::50, :, 5] = 2.0 ** 20
+    if how == "zero first":
+        v[:200] = 0.0
+    oc.append(w.pool, w.table, 32, 0, 0, k, v, 32)
+    both_cuts(w, w.normal(T, 2, dh), None)
