@@ -1,12 +1,13 @@
 // Attention of new tokens over the paged int8 cache, for few rows per key / value head and for fp32: products of whole numbers.
 //
-// The cache's codes go to the matrix cores as they are.  q is a block's power of two times a whole number of 22 (bf16) or 30 (fp32)
-// bits, and that is a sum of 3 or 4 signed bytes times 256^i: four rows of an int8 MFMA (v_mfma_i32_16x16x64_i8, whose 64 steps of
-// the contraction are exactly one block of the codec) hold one query's bytes, a tile of 16 rows four queries.  The products and their sums are
-// exact; a block's sum is put together from its bytes' sums in fp32 and multiplied by q's power of two and the keys' scales.
-// The weights p_j = 2^(s_j - m) go the same way: p_j times the value's scale, as a whole number of 22 / 30 bits relative to
-// the tile's largest scale, contracted with the value codes over 64 tokens at a time.  Nothing is converted per cached element, and
-// one query uses the matrix cores no worse than four.
+// The cache's codes go to the matrix cores as they are.  q is a block's power of two times a whole number of 30 bits, and that is a sum of 4
+// signed bytes times 256^i: four rows of an int8 MFMA (v_mfma_i32_16x16x64_i8, whose 64 steps of the contraction are exactly one block
+// of the codec) hold one query's bytes, a tile of 16 rows four queries.  The products and their sums are exact; a block's sum is put together
+// from its bytes' sums in fp32 and multiplied by q's power of two and the keys' scales.
+// The weights p_j = 2^(s_j - m) go the same way: p_j times the value's scale, as a whole number of 30 bits relative to the largest that the
+// query has among the 64 tokens, contracted with their value codes.  Where the tokens' scales lie further apart than 2^5, what those 30 bits
+// leave of a weight goes through a second time (60 bits of the largest): a value's elements are not all large, and where its code is 0 the
+// others' are all there is.  Nothing is converted per cached element, and one query uses the matrix cores no worse than four.
 //   keys    column n of tile c is token 4 n + c: a lane then holds the weights of four consecutive tokens, one word per byte row.
 //   values  lie transposed in the cache: a lane's operand is 16 consecutive tokens of one element, one load.
 // What a wavefront reads goes straight into registers, the next 64 tokens' keys while this tile's softmax runs, the next values behind its
@@ -24,6 +25,8 @@ typedef __attribute__((ext_vector_type(4))) int i32x4;
 constexpr int kThreads = 256, kWaves = 4;
 constexpr int kTile = kAttnTile;
 constexpr int kRowPitch = 20;          // 32-bit words of a row of weights' bytes: 16, and 4 against bank conflicts
+constexpr int kBits = 30;
+constexpr int kSpread = 5;             // exponents of the scales that one pass does for
 constexpr float kLog2e = 1.4426950408889634f;
 
 // Reductions over the 16 lanes of a row of the register file
@@ -39,24 +42,18 @@ __device__ __forceinline__ uint32_t umax16(uint32_t v) {
   v = max(v, turned<8>(v)); v = max(v, turned<4>(v)); v = max(v, turned<2>(v));
   return max(v, turned<1>(v));
 }
+__device__ __forceinline__ uint32_t umin16(uint32_t v) { return ~umax16(~v); }
 __device__ __forceinline__ float sum16(float v) {
   v += __uint_as_float(turned<8>(__float_as_uint(v))); v += __uint_as_float(turned<4>(__float_as_uint(v)));
   v += __uint_as_float(turned<2>(__float_as_uint(v)));
   return v + __uint_as_float(turned<1>(__float_as_uint(v)));
 }
 
-// A number below 2^BITS in magnitude as bytes: sum of (signed byte i) * 256^i.
-template <int BYTES>
-__device__ __forceinline__ uint32_t digits(int x) {
-  constexpr uint32_t h = BYTES == 4 ? 0x80808080u : 0x00808080u;
-  const uint32_t w = ((uint32_t)x + h) ^ h;
-  return BYTES == 4 ? w : w & 0x00FFFFFFu;
-}
+// A number below 2^kBits in magnitude as bytes: sum of (signed byte i) * 256^i.
+__device__ __forceinline__ uint32_t digits(int x) { return ((uint32_t)x + 0x80808080u) ^ 0x80808080u; }
 // and back, from the sums over the bytes
-template <int BYTES>
 __device__ __forceinline__ float joined(const i32x4& a) {
-  if constexpr (BYTES == 4) return fmaf((float)((a[3] << 8) + a[2]), 65536.0f, (float)((a[1] << 8) + a[0]));
-  return fmaf((float)((a[2] << 8) + a[1]), 256.0f, (float)a[0]);
+  return fmaf((float)((a[3] << 8) + a[2]), 65536.0f, (float)((a[1] << 8) + a[0]));
 }
 
 template <bool S16>
@@ -73,8 +70,6 @@ __device__ __forceinline__ float4 scales4(const void* p, size_t i) {
 // RT tiles of four rows; a row is (token t, query head of the group): r = t * group + head.
 template <typename T, int DH, int RT, bool S16>
 __global__ __launch_bounds__(kThreads) void cache_attention_bytes_kernel(AttnArgs a) {
-  constexpr int BYTES = sizeof(T) == 2 ? 3 : 4;
-  constexpr int BITS = BYTES == 4 ? 30 : 22;
   constexpr int NB = DH / 64, Q = 4 * RT, DT = DH / 16;
   constexpr int kQBytes = Q * 4 * DH, kOBytes = kWaves * Q * (DH + 2) * 4, kPBytes = kWaves * NB * 16 * kRowPitch * 4;
   __shared__ __attribute__((aligned(16))) char lds[kQBytes + kPBytes > kOBytes ? kQBytes + kPBytes : kOBytes];
@@ -114,12 +109,12 @@ __global__ __launch_bounds__(kThreads) void cache_attention_bytes_kernel(AttnArg
       const int ex = (int)(top >> 23) - 126;                  // magnitudes are below 2^ex
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        const uint32_t w = digits<BYTES>((int)rintf(ldexpf(x[u], BITS - ex)));
+        const uint32_t w = digits((int)rintf(ldexpf(x[u], kBits - ex)));
 #pragma unroll
         for (int k = 0; k < 4; ++k) qd[(q * 4 + k) * DH + blk * 64 + e * 4 + u] = (uint8_t)(w >> (8 * k));
       }
       const float c = (DH == 64 ? 0.125f : 0.08838834764831845f) * kLog2e;
-      if (e == 0) q_scale[q][blk] = top >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : ldexpf(c, ex - BITS);
+      if (e == 0) q_scale[q][blk] = top >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : ldexpf(c, ex - kBits);
     }
   }
   __syncthreads();
@@ -199,7 +194,7 @@ __global__ __launch_bounds__(kThreads) void cache_attention_bytes_kernel(AttnArg
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
           const i32x4 acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(qf[rt][blk], kv, i32x4{0, 0, 0, 0}, 0, 0, 0);
-          p[rt][c] = fmaf(joined<BYTES>(acc), k * qs[rt][blk], p[rt][c]);
+          p[rt][c] = fmaf(joined(acc), k * qs[rt][blk], p[rt][c]);
         }
       }
     }
@@ -232,31 +227,30 @@ __global__ __launch_bounds__(kThreads) void cache_attention_bytes_kernel(AttnArg
         for (int blk = 0; blk < NB; ++blk) vn[blk][c] = any[c] ? vn[blk][c] : 0.f;
       }
     }
-    // ---- the values' scales relative to a power of two that is above them all
-    float back[NB];
+    // ---- whether the values' scales lie apart
+    bool apart = false;
 #pragma unroll
     for (int blk = 0; blk < NB; ++blk) {
-      auto largest = [&] {             // none is negative, so they compare as whole numbers; what is no number comes out on top
-        return umax16(max(max(__float_as_uint(vn[blk][0]), __float_as_uint(vn[blk][1])),
-                          max(__float_as_uint(vn[blk][2]), __float_as_uint(vn[blk][3]))));
-      };
-      uint32_t top = largest();
+      uint32_t sc[4];                  // none is negative, so they compare as whole numbers; what is no number comes out on top
+#pragma unroll
+      for (int c = 0; c < 4; ++c) sc[c] = __float_as_uint(vn[blk][c]);
+      uint32_t top = umax16(max(max(sc[0], sc[1]), max(sc[2], sc[3])));
       if (__ballot(top >= 0x7F800000u)) {      // an infinite value or none: for the rows that see it, and no others
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          if (__float_as_uint(vn[blk][c]) < 0x7F800000u) continue;
+          if (sc[c] < 0x7F800000u) continue;
           vn[blk][c] = 0.f;
+          sc[c] = 0;
 #pragma unroll
           for (int rt = 0; rt < RT; ++rt)
             if (p[rt][c] != -INFINITY) l[rt] = __uint_as_float(0x7FC00000u);
         }
-        top = largest();
+        top = umax16(max(max(sc[0], sc[1]), max(sc[2], sc[3])));
       }
-      const int ex = max((int)(top >> 23) - 126, -110);        // the way back, 2^(ex - BITS), is a number
-#pragma unroll
-      for (int c = 0; c < 4; ++c) vn[blk][c] = ldexpf(vn[blk][c], BITS - ex);
-      back[blk] = ldexpf(1.0f, ex - BITS);
+      const uint32_t least = umin16(min(min(sc[0] - 1, sc[1] - 1), min(sc[2] - 1, sc[3] - 1))) + 1;      // of those that are not 0
+      apart |= top != 0 && (top >> 23) >= (least >> 23) + kSpread;
     }
+    const bool again = __ballot(apart) != 0;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       // ---- softmax of this tile
@@ -265,37 +259,54 @@ __global__ __launch_bounds__(kThreads) void cache_attention_bytes_kernel(AttnArg
       const float keep = __builtin_amdgcn_exp2f(m[rt] - top);
       m[rt] = mn;
       l[rt] *= keep;
-      uint32_t w[NB][4];
+      float w[NB][4];
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
         const float x = __builtin_amdgcn_exp2f(p[rt][c] - top);
         l[rt] += x;
 #pragma unroll
-        for (int blk = 0; blk < NB; ++blk) w[blk][c] = digits<BYTES>((int)rintf(x * vn[blk][c]));
+        for (int blk = 0; blk < NB; ++blk) w[blk][c] = x * vn[blk][c];
       }
-      // ---- byte i of four tokens to a word of row 4 q + i
+      float kept = keep;
+#pragma nounroll
+      for (int pass = 0;; ++pass) {
+        float back[NB];
 #pragma unroll
-      for (int blk = 0; blk < NB; ++blk) {
-        const uint32_t a0 = __builtin_amdgcn_perm(w[blk][1], w[blk][0], 0x05010400u), a1 = __builtin_amdgcn_perm(w[blk][3], w[blk][2], 0x05010400u);
-        const uint32_t b0 = __builtin_amdgcn_perm(w[blk][1], w[blk][0], 0x07030602u), b1 = __builtin_amdgcn_perm(w[blk][3], w[blk][2], 0x07030602u);
-        uint32_t* to = weights + blk * 16 * kRowPitch + lg * 4 * kRowPitch + n;
-        to[0] = __builtin_amdgcn_perm(a1, a0, 0x05040100u);
-        to[kRowPitch] = __builtin_amdgcn_perm(a1, a0, 0x07060302u);
-        to[2 * kRowPitch] = __builtin_amdgcn_perm(b1, b0, 0x05040100u);
-        to[3 * kRowPitch] = __builtin_amdgcn_perm(b1, b0, 0x07060302u);
-      }
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      i32x4 pf[NB];
+        for (int blk = 0; blk < NB; ++blk) {
+          const float most = max16(fmaxf(fmaxf(fabsf(w[blk][0]), fabsf(w[blk][1])), fmaxf(fabsf(w[blk][2]), fabsf(w[blk][3]))));
+          const int ex = max(__builtin_amdgcn_frexp_expf(most), -110);      // all are below 2^ex; the way back, 2^(ex - kBits), is a number
+          back[blk] = ldexpf(1.0f, ex - kBits);
+          uint32_t d[4];
 #pragma unroll
-      for (int blk = 0; blk < NB; ++blk)
-        pf[blk] = *reinterpret_cast<const i32x4*>(weights + blk * 16 * kRowPitch + n * kRowPitch + lg * 4);
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      __builtin_amdgcn_wave_barrier();
+          for (int c = 0; c < 4; ++c) {
+            const float r = rintf(ldexpf(w[blk][c], kBits - ex));
+            d[c] = digits((int)r);
+            w[blk][c] -= r * back[blk];                                     // exact
+          }
+          // byte i of four tokens to a word of row 4 q + i
+          const uint32_t a0 = __builtin_amdgcn_perm(d[1], d[0], 0x05010400u), a1 = __builtin_amdgcn_perm(d[3], d[2], 0x05010400u);
+          const uint32_t b0 = __builtin_amdgcn_perm(d[1], d[0], 0x07030602u), b1 = __builtin_amdgcn_perm(d[3], d[2], 0x07030602u);
+          uint32_t* to = weights + blk * 16 * kRowPitch + lg * 4 * kRowPitch + n;
+          to[0] = __builtin_amdgcn_perm(a1, a0, 0x05040100u);
+          to[kRowPitch] = __builtin_amdgcn_perm(a1, a0, 0x07060302u);
+          to[2 * kRowPitch] = __builtin_amdgcn_perm(b1, b0, 0x05040100u);
+          to[3 * kRowPitch] = __builtin_amdgcn_perm(b1, b0, 0x07060302u);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        i32x4 pf[NB];
 #pragma unroll
-      for (int d = 0; d < DT; ++d) {
-        const i32x4 acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(pf[d / 4], __builtin_bit_cast(i32x4, vf[d]), i32x4{0, 0, 0, 0}, 0, 0, 0);
-        o[rt][d] = fmaf(o[rt][d], keep, joined<BYTES>(acc) * back[d / 4]);
+        for (int blk = 0; blk < NB; ++blk)
+          pf[blk] = *reinterpret_cast<const i32x4*>(weights + blk * 16 * kRowPitch + n * kRowPitch + lg * 4);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          const i32x4 acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(pf[d / 4], __builtin_bit_cast(i32x4, vf[d]), i32x4{0, 0, 0, 0}, 0, 0, 0);
+          o[rt][d] = fmaf(o[rt][d], kept, joined(acc) * back[d / 4]);
+        }
+        if (__builtin_expect(!again || pass, 1)) break;
+        kept = 1.0f;
       }
     }
     if (more) {

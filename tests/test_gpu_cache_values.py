@@ -10,7 +10,6 @@ pytestmark = pytest.mark.gpu
 
 ROWS = [("f32", 64, 3), ("f32", 64, 13), ("f32", 128, 9), ("f32", 128, 40), ("bf16", 64, 3), ("bf16", 64, 7), ("bf16", 128, 3),
         ("bf16", 64, 20), ("bf16", 64, 100), ("bf16", 128, 20), ("bf16", 128, 64), ("bf16", 128, 100)]
-MANY = [(dtype, dh, T) for dtype, dh, T in ROWS if dtype == "bf16" and T > 8]
 
 
 def world(seed, dtype, dh, T, past, bits=32):
@@ -26,7 +25,7 @@ def both_cuts(w, q, words):
 
 @pytest.mark.parametrize("power", [14, 22, 30, 100])
 @pytest.mark.parametrize("past", [0, 200])
-@pytest.mark.parametrize("dtype,dh,T", MANY)
+@pytest.mark.parametrize("dtype,dh,T", ROWS)
 def test_what_a_row_does_not_see_costs_it_nothing(dtype, dh, T, past, power):
     """A later token of a prompt, or another branch of a tree, with values of another size."""
     w, q, k, v = world(8000 + T + power, dtype, dh, T, past)
@@ -42,7 +41,7 @@ def test_what_a_row_does_not_see_costs_it_nothing(dtype, dh, T, past, power):
 
 @pytest.mark.parametrize("power", [24, 60])
 @pytest.mark.parametrize("at", [3, 90, 240])
-@pytest.mark.parametrize("dtype,dh,T", MANY)
+@pytest.mark.parametrize("dtype,dh,T", ROWS)
 def test_what_a_row_sees_with_next_to_no_weight_costs_it_nothing(dtype, dh, T, at, power):
     """One token's values are 2^24 (2^60) times the others', its weight e^-60 (e^-85) of theirs."""
     n = 256
@@ -57,7 +56,7 @@ def test_what_a_row_sees_with_next_to_no_weight_costs_it_nothing(dtype, dh, T, a
     both_cuts(w, q, None)
 
 
-@pytest.mark.parametrize("dtype,dh,T", MANY)
+@pytest.mark.parametrize("dtype,dh,T", ROWS)
 @pytest.mark.parametrize("how", ["rising", "falling", "mixed", "far apart", "one element", "tiny", "zero first"])
 def test_values_of_any_size(dtype, dh, T, how):
     """Scales that change from token to token and tile to tile.  `one element`: a value is large in one place and its other codes are 0,
