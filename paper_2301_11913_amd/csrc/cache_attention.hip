@@ -235,15 +235,21 @@ __global__ __launch_bounds__(kThreads) void cache_attention_bytes_kernel(AttnArg
 #pragma unroll
       for (int c = 0; c < 4; ++c) sc[c] = __float_as_uint(vn[blk][c]);
       uint32_t top = umax16(max(max(sc[0], sc[1]), max(sc[2], sc[3])));
-      if (__ballot(top >= 0x7F800000u)) {      // an infinite value or none: for the rows that see it, and no others
+      if (__ballot(top >= 0x7F800000u)) {      // an infinite value or none: for its block of the rows that see it, and no others
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+          uint32_t hit = 0;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) hit |= sc[c] >= 0x7F800000u && p[rt][c] != -INFINITY;
+          hit = umax16(hit);
+#pragma unroll
+          for (int d = 4 * blk; d < 4 * blk + 4; ++d) o[rt][d] = hit ? __uint_as_float(0x7FC00000u) : o[rt][d];
+        }
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           if (sc[c] < 0x7F800000u) continue;
           vn[blk][c] = 0.f;
           sc[c] = 0;
-#pragma unroll
-          for (int rt = 0; rt < RT; ++rt)
-            if (p[rt][c] != -INFINITY) l[rt] = __uint_as_float(0x7FC00000u);
         }
         top = umax16(max(max(sc[0], sc[1]), max(sc[2], sc[3])));
       }

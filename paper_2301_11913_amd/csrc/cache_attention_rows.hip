@@ -320,10 +320,12 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
     for (int blk = 0; blk < NB; ++blk) vs[blk] = odd && blk != which ? st.none : st.vs[blk];
     float counted = 1.0f;                                    // what makes a weight one of the sum l
     if (odd) {
-      // a value that is infinite or none goes to all of the rows that see it, and to no others
+      // a value that is infinite or none goes to its block of all the rows that see it, and to no others
+      float none = 0.f;
       if (bad_ones) {
-        const uint32_t bad = kh == 0 ? st.about[0].y | st.about[NB - 1].y : st.about[0].z | st.about[NB - 1].z;
-        if (sees & (bad >> (8 * lh)) & 0x00FF00FFu) l = __uint_as_float(0x7FC00000u);
+        const uint32_t bad = kh == 0 ? st.about[which].y : st.about[which].z;
+        if (sees & (bad >> (8 * lh)) & 0x00FF00FFu) none = __uint_as_float(0x7FC00000u);
+        none += __shfl_xor(none, 32, 64);
       }
       // The sums to the unit, or to that of the query's largest weight here where that is less but more than the sums' own (a query
       // without weights here adds zeros in any unit); the weights to what they are in that unit.  What is too far below the sums is left out.
@@ -340,7 +342,7 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
         const int next = unit[blk], have = v_exp[blk];
         const bool first = v_top[blk] == kNoExp, counts = next >= have || next >= v_top[blk] - kFall;
         const int at = !real || (first && !any) ? next : !any || !counts ? have : next < have ? next : min(next, max(next + up, have));
-        const float less = ldexpf(1.0f, have - at);          // from no unit: 0, of sums that are 0
+        const float less = ldexpf(1.0f, have - at) + none;          // from no unit: 0, of sums that are 0
 #pragma unroll
         for (int d = 2 * blk; d < 2 * blk + 2; ++d) o[d] *= less;
         by = !any ? 0 : counts ? next - at : -60;            // 2^-60: nothing in fp16

@@ -2,7 +2,7 @@
 import numpy as np
 import pytest
 
-from cache_util import World, check_rows, tree_words
+from cache_util import RowBound, World, check_rows, seen_by_rows, tree_words
 from oracle import cache as oc
 from test_gpu_cache import ATTENTION, run_attention
 
@@ -72,3 +72,28 @@ def test_values_of_any_size(dtype, dh, T, how):
         v[:200] = 0.0
     oc.append(w.pool, w.table, 32, 0, 0, k, v, 32)
     both_cuts(w, w.normal(T, 2, dh), None)
+
+
+@pytest.mark.parametrize("bits", [32, 16])
+@pytest.mark.parametrize("bad", [np.nan, np.inf])
+@pytest.mark.parametrize("dtype,dh,T", [r for r in ROWS if r[1] == 128])
+def test_a_scale_that_is_no_number_is_its_blocks_alone(dtype, dh, T, bad, bits):
+    """One block of a value of the past (head 0) and one of a new token (head 1): NaN in that block of the rows that see it, and nowhere else."""
+    w, q, k, v = world(8600 + T, dtype, dh, T, 150, bits)
+    oc.append(w.pool, w.table, 32, 0, 150, k, v, bits)
+    at = [(0, 40, 1), (1, 150 + T // 2, 0)]                              # head, token, block
+    finite = {n: a.copy() for n, a in w.pool.items()}
+    for h, j, blk in at:
+        w.pool["v_scales"][w.table[0, j // 32], h, blk, j % 32] = bad
+        finite["v_scales"][w.table[0, j // 32], h, blk, j % 32] = 1.0
+    for max_len in (64, 1024):
+        got = run_attention(w, q, None, max_len)
+        for h, j, blk in at:
+            mine = got[0, max(0, j - 150):, h, 64 * blk:64 * blk + 64]
+            assert np.all(np.isnan(mine))
+        assert np.isnan(got).sum() == sum(64 * (T - max(0, j - 150)) for _, j, _ in at)
+        broken, w.pool = w.pool, finite
+        want = RowBound(dtype, q, *seen_by_rows(w, None, 0)).out
+        got[0] = np.where(np.isnan(got[0]), want, got[0])
+        check_rows(w, q, None, got)
+        w.pool = broken
