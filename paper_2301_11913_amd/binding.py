@@ -115,13 +115,16 @@ class CacheConfig:
         self._sizes = (batch, batch * table_pages, n_heads * d_head, n_kv_heads * d_head, self.torch_dtype)
 
     def shapes(self):
-        """Shape and dtype of the four tensors of a Cache (16-bit scales are bf16 values)."""
+        """Shape and dtype of the four tensors of a Cache (16-bit scales are bf16 values; their bit patterns as 16-bit integers do too)."""
         c = self.c
         scale = torch.float32 if c.scale_bits == 32 else torch.bfloat16
         return {"k_codes": ((c.n_pages, c.n_kv_heads, c.page_tokens, c.d_head), torch.int8),
                 "v_codes": ((c.n_pages, c.n_kv_heads, c.d_head, c.page_tokens), torch.int8),
                 "k_scales": ((c.n_pages, c.n_kv_heads, c.d_head // 64, c.page_tokens), scale),
                 "v_scales": ((c.n_pages, c.n_kv_heads, c.d_head // 64, c.page_tokens), scale)}
+
+
+_PATTERNS = tuple(getattr(torch, n) for n in ("int16", "uint16") if hasattr(torch, n))     # of bf16 values
 
 
 class Cache:
@@ -133,7 +136,7 @@ class Cache:
             t = self.tensors[name]
             if tuple(t.shape) != shape:
                 raise ValueError("%s has shape %s, the cache has %s" % (name, tuple(t.shape), shape))
-            if t.dtype != dtype and not (t.element_size() == 2 and dtype == torch.bfloat16):
+            if t.dtype != dtype and not (dtype == torch.bfloat16 and t.dtype in _PATTERNS):
                 raise TypeError("%s must be %s" % (name, dtype))
             if not t.is_contiguous():
                 raise ValueError("%s must be contiguous" % name)
