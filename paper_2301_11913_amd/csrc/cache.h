@@ -39,6 +39,17 @@ __device__ __forceinline__ size_t scales_at(const CacheArgs& a, int page, int g)
   return (((size_t)page * a.KV + g) << a.page_shift) * (DH / 64);
 }
 
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+// Values rounded to bf16 by the unit's own conversion, which leaves what is no number one whatever its bits.
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  f32x2 v = {a, b};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+}
+
+__device__ __forceinline__ void store_rounded(float* p, float v) { *p = v; }
+__device__ __forceinline__ void store_rounded(bf16_raw* p, float v) { *p = __builtin_bit_cast(bf16_raw, (__bf16)v); }
+
 // 8 consecutive elements <-> fp32
 template <typename T> struct Row8;
 template <> struct Row8<bf16_raw> {
@@ -53,8 +64,7 @@ template <> struct Row8<bf16_raw> {
   }
   static __device__ __forceinline__ void store(bf16_raw* p, const float (&x)[8]) {
     uint4 v;
-    v.x = pack_bf16x2(x[0], x[1]); v.y = pack_bf16x2(x[2], x[3]);
-    v.z = pack_bf16x2(x[4], x[5]); v.w = pack_bf16x2(x[6], x[7]);
+    v.x = pack2(x[0], x[1]); v.y = pack2(x[2], x[3]); v.z = pack2(x[4], x[5]); v.w = pack2(x[6], x[7]);
     *reinterpret_cast<uint4*>(p) = v;
   }
 };

@@ -349,8 +349,8 @@ __global__ __launch_bounds__(kThreads) void cache_attention_bytes_kernel(AttnArg
       x = fmaf(ow[(w * Q + q) * DH + d], f, x);
     }
     if (a.splits == 1) {
-      Elem<T>::store(reinterpret_cast<T*>(a.out) + ((size_t)b * a.c.tokens + r / a.group) * a.out_pitch +
-                     (size_t)(g * a.group + r % a.group) * DH + d, total == 0.f ? 0.f : x / total);
+      store_rounded(reinterpret_cast<T*>(a.out) + ((size_t)b * a.c.tokens + r / a.group) * a.out_pitch +
+                    (size_t)(g * a.group + r % a.group) * DH + d, total == 0.f ? 0.f : x / total);
     } else {
       const size_t at = (size_t)blockIdx.x * Q + q;
       a.part_o[at * DH + d] = x;
@@ -410,7 +410,7 @@ __global__ __launch_bounds__(kThreads) void cache_attention_join_kernel(AttnArgs
   const float f = total == 0.f ? 0.f : 1.0f / total;
   const float y[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) Elem<T>::store(to + i, total == 0.f ? 0.f : y[i] * f);
+  for (int i = 0; i < 4; ++i) store_rounded(to + i, total == 0.f ? 0.f : y[i] * f);
 }
 
 // How the rows and the tokens of a call are cut.

@@ -27,8 +27,6 @@ namespace swarm {
 namespace {
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
-typedef __attribute__((ext_vector_type(2))) float f32x2;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 
 constexpr float kLog2e = 1.4426950408889634f;
@@ -40,10 +38,6 @@ constexpr int kFall = 72;
 // 4 prompts of 2048 tokens, 32 heads of 128 (weights in bf16): 222 us; 4 pairs at a time 225, 2 241, one 262, all 16 of an XCD 221
 constexpr int kPairs = 8;
 
-__device__ __forceinline__ uint32_t pack2(float a, float b) {
-  f32x2 v = {a, b};
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
-}
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
 typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
 __device__ __forceinline__ uint32_t pack2_f16(float a, float b) {

@@ -1,6 +1,7 @@
 """Attention over the cache where values differ by many powers of two: every row within a bound of what that row sees."""
 import numpy as np
 import pytest
+import torch
 
 from cache_util import RowBound, World, check_rows, seen_by_rows, tree_words
 from oracle import cache as oc
@@ -97,3 +98,43 @@ def test_a_scale_that_is_no_number_is_its_blocks_alone(dtype, dh, T, bad, bits):
         got[0] = np.where(np.isnan(got[0]), want, got[0])
         check_rows(w, q, None, got)
         w.pool = broken
+
+
+@pytest.mark.parametrize("pattern", [0x7FC00000, 0x7FFFFFFF, 0xFFFFFFFF, 0x7F800001])
+@pytest.mark.parametrize("T", [1, 6, 40])
+def test_no_number_of_any_pattern_stays_one(T, pattern):
+    """fp32 scales that are NaN, whatever their bits, are NaN in bf16 too: read back, as keys and as values."""
+    import paper_2301_11913_amd as sw
+    w, q, k, v = world(8800 + T, "bf16", 64, T, 40)
+    oc.append(w.pool, w.table, 32, 0, 40, k, v, 32)
+    bad = np.array([pattern], dtype=np.uint32).view(np.float32)[0]
+    w.pool["k_scales"][w.table[0, 0], 0, 0, 7] = bad
+    w.pool["v_scales"][w.table[0, 0], 1, 0, 9] = bad
+    for max_len in (64, 1024):
+        assert np.all(np.isnan(run_attention(w, q, None, max_len)))      # head 0 by the key, head 1 by the value
+    cfg, cache = w.upload()
+    out = [torch.zeros((40, 2 * 64), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    sw.swarm_cache_read(cfg, cache, w.ints(w.table), w.ints([0]), None, 40, *out)
+    for got, token, head in ((out[0], 7, 0), (out[1], 9, 1)):
+        none = torch.isnan(got).cpu().reshape(40, 2, 64)
+        assert bool(none[token, head].all()) and int(none.sum()) == 64
+
+
+def test_read_rounds_as_torch_does():
+    """code * scale of every code, with scales of all sizes down to the smallest: the bf16 value next to the fp32 product."""
+    import paper_2301_11913_amd as sw
+    n = 512
+    cfg = sw.CacheConfig(1, 1, 64, 16, n // 16, 1, n // 16, "bf16", 32)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    pool = {name: torch.zeros(shape, dtype=dt, device="cuda") for name, (shape, dt) in cfg.shapes().items()}
+    codes = torch.randint(-127, 128, (n, 64), generator=gen, device="cuda", dtype=torch.int32).to(torch.int8)
+    scales = torch.ldexp(1 + torch.rand(n, generator=gen, device="cuda"), torch.arange(n, device="cuda") % 250 - 140)
+    pool["k_codes"].copy_(codes.reshape(n // 16, 1, 16, 64))
+    pool["v_codes"].copy_(codes.reshape(n // 16, 1, 16, 64).transpose(2, 3))
+    for name in ("k_scales", "v_scales"):
+        pool[name].copy_(scales.reshape(n // 16, 1, 1, 16))
+    out = [torch.zeros((n, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    zero = torch.zeros(1, dtype=torch.int32, device="cuda")
+    sw.swarm_cache_read(cfg, sw.Cache(cfg, **pool), torch.arange(n // 16, dtype=torch.int32, device="cuda"), zero, None, n, *out)
+    want = (codes.float() * scales[:, None]).to(torch.bfloat16)
+    assert torch.equal(out[0], want) and torch.equal(out[1], want)
