@@ -138,3 +138,36 @@ def test_read_rounds_as_torch_does():
     sw.swarm_cache_read(cfg, sw.Cache(cfg, **pool), torch.arange(n // 16, dtype=torch.int32, device="cuda"), zero, None, n, *out)
     want = (codes.float() * scales[:, None]).to(torch.bfloat16)
     assert torch.equal(out[0], want) and torch.equal(out[1], want)
+
+
+def case_world(case):
+    dtype, H, KV, dh, T, past, fresh, page, bits, tree = case
+    w = World(9000 + T + dh, dtype, H, KV, dh, T, past, page, bits, fresh)
+    for b in range(w.B):
+        n = int(w.fresh[b])
+        oc.append(w.pool, w.table, page, b, int(w.past[b]), w.normal(n, KV, dh), w.normal(n, KV, dh), bits)
+    return w, w.normal(w.B * T, H, dh, std=1.5), tree_words(w.rng, w.B, T) if tree else None
+
+
+@pytest.mark.parametrize("case", ATTENTION, ids=lambda c: "-".join(str(x) for x in c).replace(" ", ""))
+def test_every_row_within_its_own_bound(case):
+    """A bound that a tile of 64 tokens lost or counted twice exceeds, at all of these lengths."""
+    w, q, words = case_world(case)
+    for max_len in (0, 64, int((w.past + w.fresh).max())):
+        check_rows(w, q, words, run_attention(w, q, words, max_len))
+
+
+@pytest.mark.parametrize("page", [16, 128])
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("dtype,rows", [("f32", 2), ("f32", 8), ("f32", 17), ("bf16", 4), ("bf16", 5), ("bf16", 8), ("bf16", 9), ("bf16", 33),
+                                        ("bf16", 65), ("bf16", 129)])
+def test_every_number_of_rows_within_its_own_bound(dtype, rows, dh, page):
+    w, q, words = case_world((dtype, 2, 2, dh, rows, [650, 64], [rows, rows - 1], page, 32, rows <= 64))
+    for max_len in (64, 1024):
+        check_rows(w, q, words, run_attention(w, q, words, max_len))
+
+
+@pytest.mark.parametrize("dtype,T", [("f32", 3), ("bf16", 1), ("bf16", 20), ("bf16", 140)])
+def test_shared_heads_within_their_own_bounds(dtype, T):
+    w, q, words = case_world((dtype, 12, 3, 64, T, [1500, 90], None, 64, 16, T <= 64))
+    check_rows(w, q, words, run_attention(w, q, words, 2048))
