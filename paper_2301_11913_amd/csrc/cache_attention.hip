@@ -75,8 +75,9 @@ __global__ __launch_bounds__(kThreads) void cache_attention_bytes_kernel(AttnArg
   __shared__ __attribute__((aligned(16))) char lds[kQBytes + kPBytes > kOBytes ? kQBytes + kPBytes : kOBytes];
   __shared__ float q_scale[Q][NB];
   const int lane = threadIdx.x & 63, n = lane & 15, lg = lane >> 4;
-  // The same for all lanes, so that the loop over tiles is scalar.  (As a loop masked by lanes it was compiled wrongly:
-  // the values' scales were overwritten before their use.)
+  // Said to be the same for all lanes, which makes the loop over tiles a scalar one.  Without it the compiler (ROCm 7.2) masks the loop by
+  // lanes and has been seen to give the registers of the values' scales to their maximum (v_max_u32 v9, v8, v9) with the scales still to be
+  // read (v_ldexp_f32 v6, v9, v6), of source that reads one array twice and writes it nowhere between.
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int unit = blockIdx.x;
   const int split = unit % a.splits; unit /= a.splits;
@@ -423,15 +424,15 @@ struct Cut {
 Cut cut_of(const swarm_cache_config* c, int tokens, int max_len) {
   Cut k{};
   const int rows = tokens * (c->n_heads / c->n_kv_heads);
-  // bf16, 8 sequences of 4000 tokens, 32 heads, with 4 / 5 / 8 / 16 / 32 rows each: the kernel of bytes 56 / 74 / 75 / 96 / 149 us at
-  // d_head 128 and 32 / - / 34 / 62 / 96 at 64, the kernel of many rows 66 / 69 / 69 / 75 / 75 and - / - / 42 / 41 / 43
+  // bf16, 8 sequences of 4000 tokens, 32 heads, with 4 / 5 / 8 / 9 / 16 / 32 rows each: the kernel of bytes 58 / 77 / 78 / 105 / 107 / 174 us
+  // at d_head 128 and 32 / 36 / 36 / 45 / 46 / 70 at 64, the kernel of many rows 76 / 72 / 72 / 73 / 76 / 78 and 40 / 40 / 41 / 41 / 41 / 43
   k.many = c->dtype == SWARM_BF16 && rows > (c->d_head == 64 ? 8 : 4);
   if (k.many) {
     k.row_tiles = rows <= 64 ? 2 : 4;
     k.rows = 32 * k.row_tiles;
   } else {
-    // fp32, the same with 16 heads and 9 / 32 rows: tiles of 8 rows 26 / 37 us at d_head 64 and 68 / 106 at 128, of 16 rows 34 / 53 and 57 / 92
-    k.row_tiles = rows <= 4 ? 1 : rows <= 8 || c->d_head == 64 ? 2 : 4;
+    // fp32, the same with 16 heads and 9 / 32 rows: 8 rows at a time 28 / 42 us at d_head 64 and 69 / 109 at 128, 16 rows 27 / 41 and 63 / 100
+    k.row_tiles = rows <= 4 ? 1 : rows <= 8 ? 2 : 4;
     k.rows = 4 * k.row_tiles;
   }
   k.row_groups = (rows + k.rows - 1) / k.rows;
@@ -439,9 +440,9 @@ Cut cut_of(const swarm_cache_config* c, int tokens, int max_len) {
   const long long len = max_len > 0 ? std::min<long long>(max_len, cap) : cap;
   const long long tiles = (len + kTile - 1) / kTile, whole = (long long)c->batch * c->n_kv_heads * k.row_groups;
   // As many workgroups as are resident, each of four tiles at least (one for every wavefront): 512, with many rows of d_head 64 768.
-  // 32 sequences of up to 8192 tokens / one of 131072 with 8 heads: 213 / 57 us; with 1024 213 / 60, 2048 246 / 70, 4096 271 / 86.
-  // Trees of 33 over 2011 tokens, d_head 128 (weights in bf16): 43 us; with 256 50, 768 47, 1024 49.  32 rows over 8 x 4000 tokens at d_head 64: 43 us; with 512
-  // 49, 1024 53.
+  // 32 sequences of up to 8192 tokens / one of 131072 with 8 heads: 215 / 59 us; with 256 215 / 61, 1024 215 / 62, 2048 252 / 72, 4096 281 / 90.
+  // Trees of 33 over 2011 tokens / 32 rows over 8 x 4000, d_head 128: 49 / 78 us; with 256 60 / 109, 768 54 / 90, 1024 55 / 86.
+  // 32 rows over 8 x 4000 tokens at d_head 64: 43 us; with 256 70, 512 50, 1024 53.
   const long long target = k.many && c->d_head == 64 ? 768 : 512;
   const long long chunk = std::max(4ll, std::min<long long>(1ll << 24, (whole * tiles + target - 1) / target));
   k.splits = (int)std::max(1ll, (tiles + chunk - 1) / chunk);
@@ -477,7 +478,7 @@ swarm_status launch(const AttnArgs& a, const Cut& k, hipStream_t st) {
   } else {
     if constexpr (sizeof(T) == 4 || DH == 64)
       if (k.row_tiles == 2) launch_bytes<T, DH, 2>(a, (unsigned)blocks, st);
-    if constexpr (sizeof(T) == 4 && DH == 128)
+    if constexpr (sizeof(T) == 4)
       if (k.row_tiles == 4) launch_bytes<T, DH, 4>(a, (unsigned)blocks, st);
   }
   if (k.splits > 1) {

@@ -35,7 +35,7 @@ constexpr int kRange = 6;              // exponents of the scales that go togeth
 // How far below its largest weight the unit of a query's sums may be.  A weight is below 2^15 units (2^8 by the running maximum, 2^7 by the
 // scale), a code is below 2^7 and there are up to 2^30 tokens, so sums are numbers down to a unit of 2^-72 of that weight's.
 constexpr int kFall = 72;
-// 4 prompts of 2048 tokens, 32 heads of 128 (weights in bf16): 222 us; 4 pairs at a time 225, 2 241, one 262, all 16 of an XCD 221
+// 4 prompts of 2048 tokens, 32 heads of 128, on one state after the other: 265 us; 4 pairs at a time 263, 2 286, one 298, all 16 of an XCD 262
 constexpr int kPairs = 8;
 
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
