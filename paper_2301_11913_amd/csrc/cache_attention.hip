@@ -431,8 +431,9 @@ Cut cut_of(const swarm_cache_config* c, int tokens, int max_len) {
     k.row_tiles = rows <= 64 ? 2 : 4;
     k.rows = 32 * k.row_tiles;
   } else {
-    // fp32, the same with 16 heads and 9 / 32 rows: 8 rows at a time 28 / 42 us at d_head 64 and 69 / 109 at 128, 16 rows 27 / 41 and 63 / 100
-    k.row_tiles = rows <= 4 ? 1 : rows <= 8 ? 2 : 4;
+    // fp32, the same with 16 heads and 9 / 32 rows: 8 rows at a time 28 / 42 us at d_head 64 and 69 / 109 at 128, 16 rows 27 / 41 and 63 / 100;
+    // a call with 9 rows over 4 x 500 tokens, 4 heads of 64, 10.3 and 10.9
+    k.row_tiles = rows <= 4 ? 1 : rows <= 8 || c->d_head == 64 ? 2 : 4;
     k.rows = 4 * k.row_tiles;
   }
   k.row_groups = (rows + k.rows - 1) / k.rows;
@@ -478,7 +479,7 @@ swarm_status launch(const AttnArgs& a, const Cut& k, hipStream_t st) {
   } else {
     if constexpr (sizeof(T) == 4 || DH == 64)
       if (k.row_tiles == 2) launch_bytes<T, DH, 2>(a, (unsigned)blocks, st);
-    if constexpr (sizeof(T) == 4)
+    if constexpr (sizeof(T) == 4 && DH == 128)
       if (k.row_tiles == 4) launch_bytes<T, DH, 4>(a, (unsigned)blocks, st);
   }
   if (k.splits > 1) {
