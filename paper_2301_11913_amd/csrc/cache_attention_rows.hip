@@ -371,8 +371,8 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
     }
   };
 
-  if (threadIdx.x < 128) stage[threadIdx.x >> 6].none[threadIdx.x & 63] = 0.f;
-  if (first < end) {
+  if (first < end) {                     // (no write to LDS without tiles: nothing would keep it from the results that are joined there)
+    if (threadIdx.x < 128) stage[threadIdx.x >> 6].none[threadIdx.x & 63] = 0.f;
     Pages pg = pages_of(first);
     uint64_t valid = valid_of(first, pg);
     load(first, pg);

@@ -171,3 +171,18 @@ def test_every_number_of_rows_within_its_own_bound(dtype, rows, dh, page):
 def test_shared_heads_within_their_own_bounds(dtype, T):
     w, q, words = case_world((dtype, 12, 3, 64, T, [1500, 90], None, 64, 16, T <= 64))
     check_rows(w, q, words, run_attention(w, q, words, 2048))
+
+
+@pytest.mark.parametrize("dtype,dh,T", ROWS + [("bf16", 64, 40), ("bf16", 64, 64)])
+def test_scores_far_below_zero_and_splits_without_tokens(dtype, dh, T):
+    """Every score is about -300, and the short sequence leaves most of the workgroups that share its rows without a token."""
+    w = World(9300 + T, dtype, 2, 2, dh, T, [1900, 30], 32, 32)
+    q = w.normal(w.B * T, 2, dh)
+    q[..., 0] = 30.0
+    for b in range(2):
+        n = int(w.past[b]) + T
+        k = w.normal(n, 2, dh)
+        k[..., 0] = -10.0 * np.sqrt(dh)
+        oc.append(w.pool, w.table, 32, b, 0, k, w.normal(n, 2, dh), 32)
+    for max_len in (64, 2048):
+        check_rows(w, q, None, run_attention(w, q, None, max_len))
