@@ -52,7 +52,7 @@ typedef struct { int8_t *k_codes, *v_codes; void *k_scales, *v_scales; } swarm_c
  * rotary != 0: the pairs (x[2i], x[2i+1]) of every head of k are rotated by pos * 10000^(-2i/d_head) first, and so are those of q
  * (n_heads * d_head elements, the same row_pitch), which go to q_out (rows q_out_pitch apart; may be q itself).  pos =
  * positions[b * tokens + t], or past + t where positions is NULL.  Angles and products are held in
- * 64 bits and rounded once: to fp32, which the codec quantises, and to the dtype in q_out.  rotary == 0: q, q_out and positions are NULL. */
+ * 64 bits and rounded to fp32, which the codec quantises, and from there to the dtype in q_out.  rotary == 0: q, q_out and positions are NULL. */
 swarm_status swarm_cache_append(const swarm_cache_config *cfg, const swarm_cache *cache, const int32_t *page_table,
                                 const int32_t *past, const int32_t *fresh, int32_t tokens, const void *q, const void *k,
                                 const void *v, size_t row_pitch, const int32_t *positions, int32_t rotary, void *q_out,

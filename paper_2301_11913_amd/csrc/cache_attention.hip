@@ -12,8 +12,8 @@
 //   values  lie transposed in the cache: a lane's operand is 16 consecutive tokens of one element, one load.
 // What a wavefront reads goes straight into registers, the next 64 tokens' keys while this tile's softmax runs, the next values behind its
 // last product.  Bound by reading the cache while a key / value head has few rows: 17 KB per 64 tokens at d_head 128 against
-// 400 vector instructions for four rows (32 sequences of up to 8192 tokens, 32 heads of 128: 1.26 GB in 215 us, 5.9 TB/s; the vector
-// units are busy for a quarter of that).  The four wavefronts of a workgroup take tiles in turn; long sequences are spread over
+// 506 vector instructions for four rows (32 sequences of up to 8192 tokens, 32 heads of 128: 1.26 GB in 215 us, 5.9 TB/s; the vector
+// units are busy for 30 % of that).  The four wavefronts of a workgroup take tiles in turn; long sequences are spread over
 // workgroups (splits of `chunk` tiles), whose partial sums a second kernel joins.
 #include "cache_attention.h"
 

@@ -16,8 +16,8 @@
 //           V^T as it lies.
 // RW wavefronts of a workgroup take 32 rows each; with KW = 2 two wavefronts share rows and take 32 of a tile's 64 tokens each
 // (few rows, where the tile's conversion and the wait for it would outweigh them), joined at the end.
-// 4 prompts of 2048 tokens, 32 heads of 128: 222 to 230 us, 600 to 620 TFLOP/s; 472 vector instructions per wavefront and tile keep the
-// vector units busy for 56 % of that, the products the matrix cores for 27 %, and two wavefronts per SIMD (238 registers) overlap little of
+// 4 prompts of 2048 tokens, 32 heads of 128: 224 to 238 us, 578 to 615 TFLOP/s; 461 vector instructions per wavefront and tile keep the
+// vector units busy for 54 % of that, the products the matrix cores for 27 %, and two wavefronts per SIMD (240 registers) overlap little of
 // the two.
 // The running maximum is raised only when a score passes it by 2^8.  LDS holds two stages; 16-byte chunks are XOR-swizzled so that the 16
 // rows of a fragment that are read together fall on different banks.
