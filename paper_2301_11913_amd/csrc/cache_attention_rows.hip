@@ -4,11 +4,13 @@
 // into LDS the keys turn into bf16, as the queries are, and the values into fp16.  The products are v_mfma_f32_32x32x16.  The scales never
 // touch the codes: a score is the sum over the blocks of 64 elements of (products) * (key's scale), and the weight of a value is p_j times
 // its scale, so the only roundings beyond fp32 are those of the weights.  These are held in fp16 (a rounding of 2^-11, where bf16's 2^-8 would
-// be as large as the output's own) relative to a power of two, which is the unit of the query's sums as well.  The unit puts the scales
-// between 2 and 2^7, so a weight has an error of half an fp16 step or of 2^-26 of what it would be with p_j = 1, whichever is more.  It
-// follows the tiles up and down, up no further than a query's own weights ask for.  A tile whose scales other than 0 lie further apart than
-// 2^6 is gone through once for each range of 2^6 that it has tokens in.  So a value that a row does not see, or sees with next to no weight,
+// be as large as the output's own) relative to a power of two, which is the unit of the query's sums as well.  The unit puts a tile's scales
+// between 2^-3 and 2^7, the largest from 4 on, so a weight has an error of half an fp16 step or, if that is more, of 2^-27 of what it would
+// be with p_j = 1 and the largest scale (2^-22 of that with its own scale, where that is the smallest possible).  The unit follows the tiles
+// up and down, up no further than a query's own weights ask for.  A tile whose scales other than 0 lie further apart than 2^10 is gone
+// through once for each range of 2^10 that a block has tokens in.  So a value that a row does not see, or sees with next to no weight,
 // costs the others none of their digits.
+// 4 prompts of 2048 tokens, 32 heads of 128, on one state after the other: 273 us, with scales times a random 2^+-3 274, 2^+-12 1950.
 //   scores  S^T [token][query] = K Q^T, 32 tokens x 32 queries: a lane owns one query column, so a maximum or a sum needs one exchange
 //           between lanes; row 8 a + 4 b + i of the keys' operand is token 16 (a / 2) + 8 b + 4 (a % 2) + i, which leaves a lane eight
 //           consecutive tokens' weights twice:
@@ -31,7 +33,8 @@ typedef __attribute__((ext_vector_type(16))) float f32x16;
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kNoExp = -100000;        // no unit yet
-constexpr int kRange = 6;              // exponents of the scales that go together
+constexpr int kRange = 10;             // exponents of the scales that go together: 2^-3 to 2^7 units
+constexpr int kLeast = 124;            // the biased exponent of a scale of 2^-3 units, less the unit's exponent
 // How far below its largest weight the unit of a query's sums may be.  A weight is below 2^15 units (2^8 by the running maximum, 2^7 by the
 // scale), a code is below 2^7 and there are up to 2^30 tokens, so sums are numbers down to a unit of 2^-72 of that weight's.
 constexpr int kFall = 72;
@@ -235,14 +238,14 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
       const uint64_t bad = __ballot(there && !fine);
       const float v = there && fine ? sc : 0.f;
       const uint32_t bits = __float_as_uint(v) & 0x7FFFFFFFu;
-      const int ex = (int)(bits >> 23);                      // v is from 2^(ex - 127) to below 2^(ex - 126)
+      const int ex = (int)(bits >> 23), place = ex - kLeast - v_now;       // v is from 2^(ex - 127) to below 2^(ex - 126)
       bool apart = false;
-      if (__ballot(bits != 0 && (uint32_t)(ex - 128 - v_now) >= (uint32_t)kRange)) {
+      if (__ballot(bits != 0 && (uint32_t)place >= (uint32_t)kRange) || (__ballot(place >= kRange / 2) == 0 && __ballot(bits != 0))) {
         const int hi = (int)(wave_umax(bits) >> 23), lo = (int)((wave_umin(bits - 1) + 1) >> 23);    // of those that are not 0
         apart = lo == 0 || hi - lo >= kRange;
-        if (!apart) v_now = lo - 128 - (kRange - 1 - (hi - lo)) / 2;
+        if (!apart) v_now = (hi - lo == kRange - 1 ? hi : hi + 1) - kRange + 1 - kLeast;        // room for a scale twice as large, if there is
       }
-      const int unit = apart && bits != 0 ? ex - ex % kRange - 128 : v_now;
+      const int unit = apart && bits != 0 ? ex - ex % kRange - kLeast : v_now;
       st.vs[blk][key] = ldexpf(v, -unit);
       if (apart) st.unit[blk][key] = unit;
       if (key == 0) st.about[blk] = make_uint4((uint32_t)(v_now * 4 + (apart ? 2 : 0) + (bad ? 1 : 0)), (uint32_t)bad, (uint32_t)(bad >> 32), 0);
@@ -251,8 +254,9 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
 
   // 32 tokens of a tile: scores, weights, output
   const int k_row = (n & 16) | ((n & 4) << 1) | ((n & 8) >> 1) | (n & 3);       // the token of this lane's row of the keys' operand
-  // odd: not all queries' sums are in the tile's unit(s), or there is a bad value: for the block `which` alone then
-  auto half = [&](const St& st, int j0, int kh, uint64_t valid, const int (&unit)[NB], bool odd, int which, bool bad_ones) {
+  // odd: not all queries' sums are in the tile's unit, or it has several, or there is a bad value: for the block `which` alone then, and
+  // tokens of one unit
+  auto half = [&](const St& st, int j0, int kh, uint64_t valid, bool odd, int which, int unit, bool bad_ones) {
     f32x16 acc[NB];
 #pragma unroll
     for (int blk = 0; blk < NB; ++blk)
@@ -333,7 +337,7 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
 #pragma unroll
       for (int blk = 0; blk < NB; ++blk) {
         if (blk != which) continue;
-        const int next = unit[blk], have = v_exp[blk];
+        const int next = unit, have = v_exp[blk];
         const bool first = v_top[blk] == kNoExp, counts = next >= have || next >= v_top[blk] - kFall;
         const int at = !real || (first && !any) ? next : !any || !counts ? have : next < have ? next : min(next, max(next + up, have));
         const float less = ldexpf(1.0f, have - at) + none;          // from no unit: 0, of sums that are 0
@@ -392,47 +396,47 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
         if (tile + 2 < end) pg = pages_of(tile + 2);
       }
       const int j0 = tile * kAttnTile;
-      int unit[NB], flags = 0;
+      int flags = 0;
       bool moves = false;
 #pragma unroll
       for (int blk = 0; blk < NB; ++blk) {
         head[blk] = __builtin_amdgcn_readfirstlane(head[blk]);
         flags |= head[blk] & 3;
-        unit[blk] = head[blk] >> 2;
-        if (tile == first && !(head[blk] & 2)) v_exp[blk] = unit[blk];          // of sums that are 0 yet
-        moves |= v_exp[blk] != unit[blk];
+        if (tile == first && !(head[blk] & 2)) v_exp[blk] = head[blk] >> 2;     // of sums that are 0 yet
+        moves |= v_exp[blk] != head[blk] >> 2;
       }
       const bool odd = flags != 0 || __ballot(moves) != 0;
       if (__builtin_expect(!odd, 1)) {
         if constexpr (KW == 1) {
-          if (j0 < outer) half(st, j0, 0, valid, unit, false, 0, false);
-          if (j0 + 32 < outer) half(st, j0, 1, valid, unit, false, 0, false);
+          if (j0 < outer) half(st, j0, 0, valid, false, 0, 0, false);
+          if (j0 + 32 < outer) half(st, j0, 1, valid, false, 0, 0, false);
         } else {
-          if (j0 + 32 * key_wave < outer) half(st, j0, key_wave, valid, unit, false, 0, false);
+          if (j0 + 32 * key_wave < outer) half(st, j0, key_wave, valid, false, 0, 0, false);
         }
       }
-      // for both blocks in turn, for every pair of units there is; the tokens that are left are the same for all lanes, as the loop has to know
-      uint64_t rest = !odd ? 0 : (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(valid >> 32)) << 32 |
-                                 (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)valid);
+#pragma unroll
+      for (int blk = 0; blk < NB; ++blk) v_top[blk] = odd && most > -INFINITY ? max(v_top[blk], v_exp[blk]) : v_top[blk];
 #pragma nounroll
-      while (__builtin_expect(rest != 0, 0)) {
-#pragma unroll
-        for (int blk = 0; blk < NB; ++blk) v_top[blk] = most == -INFINITY ? v_top[blk] : max(v_top[blk], v_exp[blk]);
-        uint64_t now = rest;
-        if (flags & 2) {
-          const int of = __builtin_ctzll(rest);
-#pragma unroll
-          for (int blk = 0; blk < NB; ++blk) {
-            const int mine = head[blk] & 2 ? st.unit[blk][lane] : unit[blk];
-            unit[blk] = __builtin_amdgcn_readlane(mine, of);
-            now &= __ballot(mine == unit[blk]);
+      for (int which = 0; __builtin_expect(odd && which < NB, 0); ++which) {
+        const int mine = which == 0 ? head[0] : head[NB - 1];
+        // the tokens that are left; the same for all lanes, as the loop over their units has to know
+        uint64_t rest = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(valid >> 32)) << 32 |
+                        (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)valid);
+#pragma nounroll
+        while (rest) {
+          uint64_t now = rest;
+          int unit = mine >> 2;
+          if (mine & 2) {
+            const int theirs = st.unit[which][lane];
+            unit = __builtin_amdgcn_readlane(theirs, __builtin_ctzll(rest));
+            now &= __ballot(theirs == unit);
           }
-        }
-        rest &= ~now;
+          rest &= ~now;
 #pragma nounroll
-        for (int i = 0; i < NB * (KW == 1 ? 2 : 1); ++i) {
-          const int kh = KW == 1 ? i & 1 : key_wave;
-          if (j0 + 32 * kh < outer) half(st, j0, kh, now, unit, true, KW == 1 ? i >> 1 : i, flags & 1);
+          for (int i = 0; i < (KW == 1 ? 2 : 1); ++i) {
+            const int kh = KW == 1 ? i : key_wave;
+            if (j0 + 32 * kh < outer) half(st, j0, kh, now, true, which, unit, flags & 1);
+          }
         }
       }
       if (more) store(stage[(tile + 1 - first) & 1], valid_next);

@@ -101,9 +101,9 @@ class RowBound:
                                  running sums one rounding per 64 tokens and 64 for the rest.  Numerator and denominator carry it
       2^-11 p_j |v_j|            bf16: a weight is rounded to 11 bits, half a step off at most, up or down by chance: the sum of n such errors
                                  is below 7 times the root of the sum of their squares but for 2 exp(-49 / 2) of all cases
-      2^-26 |v_j|                or, where that is more, it is held to 2^-26 of what the value would have with the weight 1; to 2^-24 of the
-                                 largest of all weights times scales where that is less
-      2^-56 of that largest      a weight times its scale may be left out below (include/swarm_cache.h), times a code
+      2^-22 |v_j|                bf16; fp32 2^-26.  Or, where that is more, it is held to this part of what the value would have with the weight
+                                 1; to twice (fp32 four times) this part of the largest of all weights times scales where that is less
+      2^-50 of that largest      a weight times its scale may be left out below (include/swarm_cache.h), times a code
     each over L, then half a step of the type, and its smallest numbers."""
 
     def __init__(self, dtype, q, k, v, see):
@@ -126,8 +126,9 @@ class RowBound:
             for i in range(0, dh, 64):
                 scale = a[:, i:i + 64].max(axis=1, keepdims=True) / 127
                 most = np.where(see, p * scale.T, 0.0).max(axis=1, keepdims=True, initial=0.0)
-                part = np.minimum(1.0, 4.0 * most / np.where(scale == 0, 1.0, scale).T)              # [rows, tokens]
-                off[:, i:i + 64] += 2.0 ** -26 * np.where(see, part, 0.0) @ a[:, i:i + 64] + 127 * 2.0 ** -56 * most * see.sum(1, keepdims=True)
+                part = np.minimum(1.0, (2.0 if dtype == "bf16" else 4.0) * most / np.where(scale == 0, 1.0, scale).T)      # [rows, tokens]
+                off[:, i:i + 64] += (2.0 ** -22 if dtype == "bf16" else 2.0 ** -26) * np.where(see, part, 0.0) @ a[:, i:i + 64]
+                off[:, i:i + 64] += 127 * 2.0 ** -50 * most * see.sum(1, keepdims=True)
             off /= total
             self.out[:, h] = (p @ v[:, g]) / total
             self.bound[:, h] = 1.01 * off + HALF_STEP[dtype] * np.abs(self.out[:, h]) + (2.0 ** -133 if dtype == "bf16" else 2.0 ** -140)
