@@ -232,9 +232,9 @@ __global__ __launch_bounds__(kThreads) void cache_attention_bytes_kernel(AttnArg
     bool apart = false;
 #pragma unroll
     for (int blk = 0; blk < NB; ++blk) {
-      uint32_t sc[4];                  // none is negative, so they compare as whole numbers; what is no number comes out on top
+      uint32_t sc[4];                  // magnitudes compare as whole numbers; what is no number comes out on top
 #pragma unroll
-      for (int c = 0; c < 4; ++c) sc[c] = __float_as_uint(vn[blk][c]);
+      for (int c = 0; c < 4; ++c) sc[c] = __float_as_uint(vn[blk][c]) & 0x7FFFFFFFu;
       uint32_t top = umax16(max(max(sc[0], sc[1]), max(sc[2], sc[3])));
       if (__ballot(top >= 0x7F800000u)) {      // an infinite value or none: for its block of the rows that see it, and no others
 #pragma unroll

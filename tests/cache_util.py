@@ -101,8 +101,8 @@ class RowBound:
                                  running sums one rounding per 64 tokens and 64 for the rest.  Numerator and denominator carry it
       2^-11 p_j |v_j|            bf16: a weight is rounded to 11 bits, half a step off at most, up or down by chance: the sum of n such errors
                                  is below 7 times the root of the sum of their squares but for 2 exp(-49 / 2) of all cases
-      2^-22 |v_j|                bf16; fp32 2^-26.  Or, where that is more, it is held to this part of what the value would have with the weight
-                                 1; to twice (fp32 four times) this part of the largest of all weights times scales where that is less
+      2^-22 |v_j|                bf16 (half of fp16's smallest step is 2^-25 units, the smallest scale 2^-3 units); fp32 2^-26.  Or, where that
+                                 is more, it is held to this part of what the value would have with the weight 1; to twice (fp32 four times) this part of the largest of all weights times scales where that is less
       2^-50 of that largest      a weight times its scale may be left out below (include/swarm_cache.h), times a code
     each over L, then half a step of the type, and its smallest numbers."""
 

@@ -186,3 +186,16 @@ def test_scores_far_below_zero_and_splits_without_tokens(dtype, dh, T):
         oc.append(w.pool, w.table, 32, b, 0, k, w.normal(n, 2, dh), 32)
     for max_len in (64, 2048):
         check_rows(w, q, None, run_attention(w, q, None, max_len))
+
+
+@pytest.mark.parametrize("bits", [32, 16])
+@pytest.mark.parametrize("dtype,dh,T", ROWS)
+def test_scales_of_either_sign(dtype, dh, T, bits):
+    """A pool that another quantiser filled: scales below zero, and zeros of both signs."""
+    w, q, k, v = world(9500 + T, dtype, dh, T, 150, bits)
+    oc.append(w.pool, w.table, 32, 0, 150, k, v, bits)
+    for name in ("k_scales", "v_scales"):
+        a = w.pool[name]
+        a *= np.where(w.rng.random(a.shape) < 0.5, -1.0, 1.0).astype(np.float32)
+        a[w.rng.random(a.shape) < 0.1] = -0.0
+    both_cuts(w, q, None)
