@@ -77,8 +77,9 @@ swarm_status swarm_cache_keep(const swarm_cache_config *cfg, const swarm_cache *
  *     out = sum_j p_j v_j / sum_j p_j,   p_j = exp(q . k_j / sqrt(d_head)),
  * over the tokens j < past, and over those new tokens u < fresh (j = past + u) that tree[b * tokens + t] has bit u set for; tree NULL:
  * u <= t.  With a tree, tokens <= 64; tokens * n_heads / n_kv_heads <= 2^24.  A row that sees no token at all is zeros.
- * What a row does not see has no part in it.  Of what it sees, p_j times a value's scale may be left out of the sum of v_j where it is
- * below 2^-50 of the row's largest in that block of 64 elements.  A value's scale that is infinite or no number makes that block NaN in
+ * What a row does not see has no part in it.  Sums are held in 32 bits.  In bf16 a p_j may be off by 2^-11 of itself or by 2^-22 of the row's
+ * largest, whichever is more, in the sum of v_j.  p_j times a value's scale may be left out there where it is below 2^-50 of the row's
+ * largest in that block of 64 elements.  A value's scale that is infinite or no number makes that block NaN in
  * the rows that see it; a key's scale or an element of q that is makes the row NaN.
  * q rows (n_heads * d_head elements) are q_pitch apart, out rows out_pitch.  max_len: a bound on past + fresh that the caller knows
  * (0: what page_table can hold); it decides over how many workgroups a sequence is spread, and the workspace; a longer sequence

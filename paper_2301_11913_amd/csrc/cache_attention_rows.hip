@@ -337,10 +337,12 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
 #pragma unroll
       for (int blk = 0; blk < NB; ++blk) {
         if (blk != which) continue;
-        const int next = unit, have = v_exp[blk];
-        const bool first = v_top[blk] == kNoExp, counts = next >= have || next >= v_top[blk] - kFall;
+        const int next = unit;
+        const bool first = v_top[blk] < kNoExp / 2;          // the sums are 0 yet, in no unit
+        const int have = first ? kNoExp : v_exp[blk];
+        const bool counts = next >= have || next >= v_top[blk] - kFall;
         const int at = !real || (first && !any) ? next : !any || !counts ? have : next < have ? next : min(next, max(next + up, have));
-        const float less = ldexpf(1.0f, have - at) + none;          // from no unit: 0, of sums that are 0
+        const float less = (first ? 0.f : ldexpf(1.0f, have - at)) + none;
 #pragma unroll
         for (int d = 2 * blk; d < 2 * blk + 2; ++d) o[d] *= less;
         by = !any ? 0 : counts ? next - at : -60;            // 2^-60: nothing in fp16

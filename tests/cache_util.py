@@ -101,8 +101,11 @@ class RowBound:
                                  running sums one rounding per 64 tokens and 64 for the rest.  Numerator and denominator carry it
       2^-11 p_j |v_j|            bf16: a weight is rounded to 11 bits, half a step off at most, up or down by chance: the sum of n such errors
                                  is below 7 times the root of the sum of their squares but for 2 exp(-49 / 2) of all cases
-      2^-22 |v_j|                bf16 (half of fp16's smallest step is 2^-25 units, the smallest scale 2^-3 units); fp32 2^-26.  Or, where that
-                                 is more, it is held to this part of what the value would have with the weight 1; to twice (fp32 four times) this part of the largest of all weights times scales where that is less
+      2^-22 |v_j|                bf16: fp16's smallest step is 2^-24 units, half of it 2^-25, and the unit is no more than 2^3 of the value's
+                                 scale.  Nor is it more than 2^4 of the largest p_j times a scale M and 2^3 of the smallest scale of any
+                                 earlier tile, which is no more than the scale S that 32 of the tokens reach: 2^-25 max(2^4 M, 2^3 S) per code.
+                                 fp32: 2^-31 of the 64 tokens' largest p_j times a scale, which is 2^-26 |v_j| with scales 2^5 apart at most,
+                                 and no more than 2^-31 M per code
       2^-50 of that largest      a weight times its scale may be left out below (include/swarm_cache.h), times a code
     each over L, then half a step of the type, and its smallest numbers."""
 
@@ -126,8 +129,13 @@ class RowBound:
             for i in range(0, dh, 64):
                 scale = a[:, i:i + 64].max(axis=1, keepdims=True) / 127
                 most = np.where(see, p * scale.T, 0.0).max(axis=1, keepdims=True, initial=0.0)
-                part = np.minimum(1.0, (2.0 if dtype == "bf16" else 4.0) * most / np.where(scale == 0, 1.0, scale).T)      # [rows, tokens]
-                off[:, i:i + 64] += (2.0 ** -22 if dtype == "bf16" else 2.0 ** -26) * np.where(see, part, 0.0) @ a[:, i:i + 64]
+                seen = np.sort(np.where(see, scale.T, 0.0), axis=1)[:, ::-1]
+                common = seen[:, min(31, seen.shape[1] - 1)][:, None] if see.shape[1] >= 32 else seen[:, :1]
+                common = np.where(see.sum(1, keepdims=True) >= 32, common, seen[:, :1])
+                most_of = np.maximum(2.0 ** -21 * most, 2.0 ** -22 * common) if dtype == "bf16" else 2.0 ** -30 * most
+                own = (2.0 ** -22 if dtype == "bf16" else 2.0 ** -26) * scale.T
+                part = np.where(see, np.minimum(own, most_of) / np.where(scale == 0, 1.0, scale).T, 0.0)          # [rows, tokens]
+                off[:, i:i + 64] += part @ a[:, i:i + 64]
                 off[:, i:i + 64] += 127 * 2.0 ** -50 * most * see.sum(1, keepdims=True)
             off /= total
             self.out[:, h] = (p @ v[:, g]) / total

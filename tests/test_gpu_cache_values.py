@@ -199,3 +199,33 @@ def test_scales_of_either_sign(dtype, dh, T, bits):
         a *= np.where(w.rng.random(a.shape) < 0.5, -1.0, 1.0).astype(np.float32)
         a[w.rng.random(a.shape) < 0.1] = -0.0
     both_cuts(w, q, None)
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_anything_at_once(seed):
+    """Random shapes, trees, pages, cuts, scores some hundreds apart and values of sizes that change by token, by tile or not at all."""
+    rng = np.random.default_rng(9700 + seed)
+    dtype, dh = ("bf16", "bf16", "f32")[seed % 3], (64, 128)[seed // 3 % 2]
+    T, KV, group = int(rng.choice([1, 2, 5, 9, 17, 33, 40, 64, 100, 150])), int(rng.integers(1, 4)), int(rng.choice([1, 1, 2, 4]))
+    past = [int(x) for x in rng.integers(0, 700, 3)]
+    fresh = [T, int(rng.integers(0, T + 1)), int(rng.integers(1, T + 1))]
+    page = int(rng.choice([16, 32, 64, 128]))
+    w = World(9800 + seed, dtype, KV * group, KV, dh, T, past, page, int(rng.choice([16, 32])), fresh)
+    q = w.normal(3 * T, KV * group, dh) * 2.0 ** rng.integers(-3, 4)
+    for b in range(3):
+        n = past[b] + fresh[b]
+        if n == 0:
+            continue
+        size = [np.zeros(n), rng.uniform(-3, 3, n), rng.uniform(-20, 20, n), np.repeat(rng.uniform(-30, 30, n // 64 + 1), 64)[:n],
+                rng.choice([0.0, 0.0, 0.0, -12.0, 25.0], n)][int(rng.integers(0, 5))]
+        v = w.normal(n, KV, dh) * 2.0 ** size[:, None, None]
+        if dh == 128 and rng.random() < 0.5:                             # the second block's sizes go another way
+            v[..., 64:] = w.normal(n, KV, 64) * 2.0 ** -size[:, None, None]
+        v[rng.random(n) < 0.05] = 0.0
+        k = w.normal(n, KV, dh) * rng.choice([0.1, 1.0, 4.0])
+        oc.append(w.pool, w.table, page, b, 0, k, v, w.scale_bits)
+    words = tree_words(w.rng, 3, T) if T <= 64 and rng.random() < 0.6 else None
+    if words is not None and rng.random() < 0.5:
+        words &= w.rng.integers(0, 1 << 63, words.shape, dtype=np.uint64) * np.uint64(2) + np.uint64(1)     # holes, some rows blind of themselves
+    for max_len in (0, 64, 700 + T):
+        check_rows(w, q, words, run_attention(w, q, words, max_len))
