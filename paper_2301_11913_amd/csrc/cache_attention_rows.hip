@@ -327,9 +327,10 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
       }
       // The sums to the unit, or to that of the query's largest weight here where that is less but more than the sums' own (a query
       // without weights here adds zeros in any unit); the weights to what they are in that unit.  What is too far below the sums is left out.
-      float top = p[0];
+      const float* mine = which == 0 ? st.vs[0] : st.vs[NB - 1];
+      float top = -INFINITY;                                 // of those that have a value other than 0
 #pragma unroll
-      for (int e = 1; e < 16; ++e) top = fmaxf(top, p[e]);
+      for (int e = 0; e < 16; ++e) top = fmaxf(top, mine[32 * kh + 16 * (e >> 3) + 8 * lh + (e & 7)] != 0.f ? p[e] : -INFINITY);
       top = fmaxf(top, __shfl_xor(top, 32, 64));
       const bool any = top > -126.0f;
       const int up = (int)ceilf(any ? top : 0.f);            // the weights are 2^up at most
@@ -341,7 +342,7 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void cache_attention_rows_kernel(A
         const bool first = v_top[blk] < kNoExp / 2;          // the sums are 0 yet, in no unit
         const int have = first ? kNoExp : v_exp[blk];
         const bool counts = next >= have || next >= v_top[blk] - kFall;
-        const int at = !real || (first && !any) ? next : !any || !counts ? have : next < have ? next : min(next, max(next + up, have));
+        const int at = !real || (first && !any) ? next : !any || !counts ? v_exp[blk] : next < have ? next : min(next, max(next + max(up, -100), have));
         const float less = (first ? 0.f : ldexpf(1.0f, have - at)) + none;
 #pragma unroll
         for (int d = 2 * blk; d < 2 * blk + 2; ++d) o[d] *= less;

@@ -130,8 +130,8 @@ class RowBound:
                 scale = a[:, i:i + 64].max(axis=1, keepdims=True) / 127
                 most = np.where(see, p * scale.T, 0.0).max(axis=1, keepdims=True, initial=0.0)
                 seen = np.sort(np.where(see, scale.T, 0.0), axis=1)[:, ::-1]
-                common = seen[:, min(31, seen.shape[1] - 1)][:, None] if see.shape[1] >= 32 else seen[:, :1]
-                common = np.where(see.sum(1, keepdims=True) >= 32, common, seen[:, :1])
+                common = seen[:, 31:32] if see.shape[1] >= 32 else seen[:, :1]
+                common = np.where(common == 0, seen[:, :1], common)              # fewer than 32 that are not 0
                 most_of = np.maximum(2.0 ** -21 * most, 2.0 ** -22 * common) if dtype == "bf16" else 2.0 ** -30 * most
                 own = (2.0 ** -22 if dtype == "bf16" else 2.0 ** -26) * scale.T
                 part = np.where(see, np.minimum(own, most_of) / np.where(scale == 0, 1.0, scale).T, 0.0)          # [rows, tokens]

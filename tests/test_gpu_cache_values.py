@@ -201,7 +201,7 @@ def test_scales_of_either_sign(dtype, dh, T, bits):
     both_cuts(w, q, None)
 
 
-@pytest.mark.parametrize("seed", range(24))
+@pytest.mark.parametrize("seed", list(range(24)) + [231])
 def test_anything_at_once(seed):
     """Random shapes, trees, pages, cuts, scores some hundreds apart and values of sizes that change by token, by tile or not at all."""
     rng = np.random.default_rng(9700 + seed)
