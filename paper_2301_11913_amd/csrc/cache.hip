@@ -124,6 +124,7 @@ __device__ __forceinline__ void append_values(const AppendArgs& a, int block, ui
   const int head = block % a.c.KV, rest = block / a.c.KV;
   const int b = rest / a.value_tiles, tile = rest - b * a.value_tiles;
   const Span s = span_of(a.c, b);
+  if (s.fresh == 0) return;                      // there is no nearest new token to load in place of the others
   const int base = (s.past / kTile + tile) * kTile, end = s.past + s.fresh;      // places base .. base + 63
   if (base >= end || base + kTile <= s.past) return;
   constexpr int C = DH / 8;
@@ -211,6 +212,7 @@ __device__ __forceinline__ void read_values(const ReadArgs& a, int block, uint32
   const int head = block % a.c.KV, rest = block / a.c.KV;
   const int b = rest / a.value_tiles, tile = rest - b * a.value_tiles;
   const Span s = span_of(a.c, b);
+  if (s.fresh == 0) return;
   const int base = (s.past / kTile + tile) * kTile, end = s.past + s.fresh;
   if (base >= end || base + kTile <= s.past) return;
   for (int i = threadIdx.x; i < DH * 4; i += kThreads) {

@@ -87,3 +87,35 @@ def test_a_table_that_ends_with_the_tokens(dtype, T, page):
     q = w.normal(T, 2, 64)
     for max_len in (0, 64, past + T):
         check_rows(w, q, None, run_attention(w, q, None, max_len))
+
+
+@pytest.mark.parametrize("rotary", [False, True])
+@pytest.mark.parametrize("dtype,dh", [("f32", 64), ("bf16", 64), ("bf16", 128)])
+def test_a_first_sequence_without_new_tokens(dtype, dh, rotary):
+    """fresh 0 behind a past that ends anywhere: nothing of it is read or written, and what the others append is theirs.  The values lie at the
+    start of an allocation of their own, in front of which there is nothing."""
+    import paper_2301_11913_amd as sw
+    T, KV, page = 3, 2, 16
+    w = World(31, dtype, KV, KV, dh, T, [17, 40, 63, 130], page, 32, fresh=[0, 3, 0, 2])
+    cfg, cache = w.upload()
+    x = w.normal(w.B * T, KV * dh)
+    big = torch.empty((32 << 20,), dtype=w.dev(x).dtype, device="cuda")
+    v = big[:w.B * T * KV * dh].reshape(w.B * T, KV * dh)
+    v.copy_(w.dev(x))
+    args = (cfg, cache, w.ints(w.table), w.ints(w.past), w.ints(w.fresh), T)
+    if rotary:
+        q = torch.zeros_like(v)
+        sw.swarm_cache_append(*args, v.clone(), v, q=q, q_out=q, positions=torch.zeros(w.B * T, dtype=torch.int32, device="cuda"), rotary=True)
+    else:
+        sw.swarm_cache_append(*args, v, v)
+    torch.cuda.synchronize()
+    for b in range(w.B):
+        n = int(w.fresh[b])
+        rows = x.reshape(w.B, T, KV, dh)[b, :n]
+        if n:
+            oc.append(w.pool, w.table, page, b, int(w.past[b]), rows, rows, 32)
+    assert same_pool(pool_of(cache), w.pool)
+    out = [torch.full((w.B * T, KV * dh), 7.0, dtype=v.dtype, device="cuda") for _ in range(2)]
+    sw.swarm_cache_read(*args, *out)
+    got = out[1].double().cpu().numpy().reshape(w.B, T, -1)
+    assert np.all(got[[0, 2]] == 7.0) and np.all(got[3, 2] == 7.0) and np.all(got[1] != 7.0)
